@@ -463,6 +463,179 @@ cast_status_t cast_phase_progress(const float* ref, const int* anchors, int n_an
                                   int Hg, int Wg, int D, const cast_diag_params_t* params,
                                   float* p_out, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Cached history: rotary positions, appending to a paged cache, reading pages
+ * back as history blocks, and attention over the paged cache.  The pages of a
+ * bf16 cache have the layout of K, V above (M = pages, Bv = page), so a cache
+ * whose pages are the routed blocks feeds cast_route_kv and cast_anchor_attn as
+ * it is; cast_kv_read makes such blocks from any cache, 8-bit ones included.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Rotary positions.  Of the dh channels of a head the first rot_dim turn in pairs,
+ * the rest pass through; pair j is channels (j, j + rot_dim/2), or (2j, 2j + 1)
+ * with `interleaved`.  At position p (one int32 per axis) pair (x, y) becomes
+ *   (a (x cos t - y sin t), a (x sin t + y cos t)),  t = 2 pi p[axis[j]] turns[j],
+ * with a = amplitude.  t is reduced to one revolution in fp64, so far positions
+ * lose nothing; the products are fp32, rounded once to the output's type.
+ */
+typedef struct {
+  int rot_dim;            /* rotated channels: even, 2 .. dh                           */
+  int interleaved;        /* pair layout: 0 (j, j + rot_dim/2), 1 (2j, 2j + 1)          */
+  int n_axes;             /* position components, 1 .. 3                               */
+  float amplitude;        /* cos and sin are multiplied by it (1: none)                */
+  const double* turns;    /* DEVICE fp64 [rot_dim/2], revolutions per position step     */
+  const uint8_t* axis;    /* DEVICE uint8 [rot_dim/2], position component of each pair
+                             (values past n_axes - 1 count as that); NULL: component 0 */
+} cast_rope_params_t;
+
+/* Scaling of the frequencies for contexts longer than the trained one. */
+#define CAST_ROPE_SCALE_NONE 0
+#define CAST_ROPE_SCALE_LINEAR 1   /* every frequency / factor                           */
+#define CAST_ROPE_SCALE_PARTS 2    /* by parts (arXiv 2309.00071): frequency times
+                                      g + (1 - g) / factor, g = clamp((orig_len turns -
+                                      beta_slow) / (beta_fast - beta_slow), 0, 1)        */
+
+/*
+ * Host helper: the frequency and axis tables of cast_rope_params_t, to be copied to the
+ * device once per model.  The rot_dim = sum of axis_dims channels are shared out over
+ * the axes in order; pair i of an axis of d channels turns base^(-2i/d) / (2 pi)
+ * revolutions per step, then scaled.
+ * axis_dims  HOST int[n_axes], each even and >= 2, sum <= 128; 1 <= n_axes <= 3.
+ * base > 0; scaling one of the above; factor >= 1 (not read for NONE); orig_len > 0 and
+ * beta_fast > beta_slow >= 0 (PARTS only).
+ * turns_out  HOST double[rot_dim/2];  axis_out  HOST uint8[rot_dim/2].
+ */
+cast_status_t cast_rope_frequencies(const int* axis_dims, int n_axes, double base, int scaling,
+                                    double factor, double orig_len, double beta_fast,
+                                    double beta_slow, double* turns_out, uint8_t* axis_out);
+
+/*
+ * out[t, h, :] = rotation of x[t, h, :] at positions pos[t, :].
+ * x, out   device, dtype (0: fp32, 1: bf16); element (t, h, c) at t * token_stride +
+ *          h * head_stride + c (strides in elements, both >= dh, any order).  `out` may be
+ *          x itself with the same strides; otherwise they must not overlap.  Aligned to
+ *          their element; 16-byte aligned buffers and strides take the fast path.
+ * pos      device int32 [n, n_axes], any values.
+ * transpose  0, or 1: turn by -t (same amplitude).  That is the transposed matrix: it
+ *          carries the gradient of the rotation, and with amplitude 1 undoes it.
+ * n >= 0 (0: nothing is enqueued), H >= 1, dh in {32, 64, 128}; n * H * dh < 2^40.
+ * Errors: CAST_ERR_NULL, CAST_ERR_SHAPE (sizes, dtype, strides under which the elements
+ * of `out` would meet, out == x with other strides, alignment), CAST_ERR_UNSUPPORTED (dh).
+ */
+cast_status_t cast_rope(const void* x, int dtype, int n, int H, int dh, long long x_token_stride,
+                        long long x_head_stride, const int32_t* pos,
+                        const cast_rope_params_t* params, int transpose, void* out,
+                        long long out_token_stride, long long out_head_stride,
+                        hipStream_t stream);
+
+/*
+ * A paged cache.  dtype 1: bf16 values.  dtype 2: e4m3 codes (OCP, 1-4-3 bits) with one
+ * exponent byte per (page, head), value = code * 2^(byte - 127).  The scales are powers
+ * of two, so every value of an 8-bit cache is a bf16 number exactly.
+ */
+typedef struct {
+  void* k;                /* device [pages, page, H, dh] bf16 or uint8 codes            */
+  void* v;
+  uint8_t* k_exp;         /* device [pages, H], dtype 2 only (else NULL)                */
+  uint8_t* v_exp;
+  int dtype;              /* 1: bf16, 2: e4m3                                          */
+  int pages, page;        /* number of pages, tokens per page                          */
+  int H, dh;              /* KV heads; dh in {32, 64, 128}                             */
+} cast_kv_cache_t;
+
+/*
+ * A ragged batch of sequences over a cache.  Sequence b owns rows cu[b] .. cu[b+1] of a
+ * call's tokens; they are the LAST of its len[b] tokens, so row r is token
+ * len[b] - (cu[b+1] - r) of its sequence.  Token t lies in page table[b, t / page] at row
+ * t % page.  Everything is read on the device when the call runs: a captured graph follows
+ * new lengths and tables.  Rows of a call behind cu[n_seq] belong to no sequence; outputs
+ * there are left as they were.  Entries of the table outside [0, pages) name no page: what
+ * would be stored there is dropped, keys there are invisible.
+ */
+typedef struct {
+  const int32_t* cu;      /* device int32 [n_seq + 1], not decreasing, in [0, n_tok]   */
+  const int32_t* len;     /* device int32 [n_seq], lengths WITH the call's tokens       */
+  const int32_t* table;   /* device int32 [n_seq, max_pages]                           */
+  int n_seq, n_tok;       /* sequences; rows of the call's tensors                     */
+  int max_pages;          /* columns of the table; lengths count up to max_pages * page */
+} cast_kv_seqs_t;
+
+/*
+ * Store the keys and values of a call's tokens, keys rotated on the way, and rotate the
+ * call's queries in the same launch.
+ *
+ * k, v     bf16 [n_tok, H, dh] device; token t at t * stride elements (>= H * dh, multiple
+ *          of 8), heads dense.
+ * rope     NULL: keys are stored as they come (and q must be NULL).
+ * pos      device int32 [n_tok, n_axes], or NULL: the token's index in its sequence
+ *          (n_axes = 1).  Read only with rope.
+ * q        bf16 [n_tok, Hq, dh] device like k (q_stride), or NULL; q_out bf16 [n_tok, Hq, dh]
+ *          device, dense, q itself where q_stride = Hq * dh.
+ * An 8-bit cache rounds (to nearest even) value * 2^-e, e the least exponent >= -117 with
+ * |value| * 2^-e <= 448 over the page's tokens of the head.  While a page holds earlier
+ * tokens of the sequence its exponent only grows; when it does the earlier codes are
+ * rounded again to the new one, which changes only those that become subnormal.  NaN and
+ * infinities do not count for e and are stored as NaN.
+ * A page may be written by one sequence of a call only (two give unspecified values in
+ * that page, nothing outside it); rows of a page behind the last token are not touched.
+ * Tensors must not overlap the cache.  n_seq >= 1, n_tok >= 0 (0: nothing is enqueued);
+ * 16-byte aligned tensors (int32 ones 4-byte); H <= 4096, page < 2^24,
+ * pages * page < 2^31, page * H * H < 2^40; n_seq <= 2^20, n_tok < 2^30, max_pages < 2^24,
+ * max_pages * page < 2^30, max_pages * page * page and n_tok * page < 2^40, n_tok < 2^24 page
+ * (the same limits hold for every call on a cache).
+ * Errors: CAST_ERR_NULL, CAST_ERR_SHAPE, CAST_ERR_UNSUPPORTED (dh; sizes past the limits).
+ */
+cast_status_t cast_kv_append(const cast_kv_cache_t* cache, const cast_kv_seqs_t* seqs,
+                             const void* k, long long k_stride, const void* v, long long v_stride,
+                             const cast_rope_params_t* rope, const int32_t* pos,
+                             const void* q, long long q_stride, int Hq, void* q_out,
+                             hipStream_t stream);
+
+/*
+ * Pages of a cache as bf16 history blocks: k_out[i] = K of page page_idx[i], v_out likewise.
+ * page_idx  device int32 [m]; an entry outside [0, pages) gives a block of zeros.
+ * k_out, v_out  bf16 [m, page, H, dh] device, 16-byte aligned; one of them may be NULL.
+ * m >= 0 (0: nothing is enqueued).  Values of an 8-bit cache come out exactly.
+ */
+cast_status_t cast_kv_read(const cast_kv_cache_t* cache, const int32_t* page_idx, int m,
+                           void* k_out, void* v_out, hipStream_t stream);
+
+/*
+ * Device scratch with which cast_kv_attn splits long key ranges over more workgroups
+ * (0: these sizes run whole).  It does not fall as max_len grows.  Reads only the sizes
+ * of the structs.
+ */
+size_t cast_kv_attn_workspace_bytes(const cast_kv_cache_t* cache, const cast_kv_seqs_t* seqs,
+                                    int Hq, int max_len, int causal, int window, int sinks);
+
+/*
+ * Attention of a call's queries over the paged cache.  Query row r, token p of sequence b,
+ * head h reads KV head h / (Hq / H):
+ *   out[r, h, :] = softmax_j(scale * q[r, h, :] . K_j) V_j over the visible keys j of b:
+ *     j < len[b],  j <= p if causal,  and with window > 0: j > p - window or j < sinks
+ * (a window of the past: without `causal` the keys after p stay visible), and j's page is in
+ * the cache.  A row that sees no key gives 0 (log-sum-exp -inf).  What lies at invisible
+ * places, infinities and NaN included, does not reach the row.  fp32 logits, softmax and
+ * sums; probabilities are rounded to bf16 for the second product; bf16 output.
+ *
+ * q        bf16 [n_tok, Hq, dh] device; token t at t * q_stride elements (>= Hq * dh, multiple
+ *          of 8), heads dense.  Hq a multiple of cache->H.
+ * out      bf16 [n_tok, Hq, dh] device, dense (must not alias the inputs).
+ * lse_out  fp32 [n_tok, Hq] device, natural log-sum-exp of the scaled logits, or NULL.
+ * max_len  the longest length expected: it sets how finely keys are split, nothing else
+ *          (longer sequences are computed, too, in longer pieces).  >= 1.
+ * window >= 0 (0: no window), sinks >= 0; scale finite and > 0.
+ * workspace  NULL (every row tile runs whole), or 256-byte aligned with
+ *          cast_kv_attn_workspace_bytes(...) of the same arguments; contents need no
+ *          initialisation.  Calls that may overlap in time need workspaces of their own.
+ * Errors: CAST_ERR_NULL, CAST_ERR_SHAPE, CAST_ERR_UNSUPPORTED, CAST_ERR_WORKSPACE.
+ */
+cast_status_t cast_kv_attn(const void* q, long long q_stride, int Hq, const cast_kv_cache_t* cache,
+                           const cast_kv_seqs_t* seqs, int max_len, int causal, int window,
+                           int sinks, float scale, void* out, float* lse_out, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,7 +30,8 @@ EXPORTED = ["cast_status_string", "cast_last_error_detail", "cast_abi_version",
             "cast_route_coupled", "cast_select_params_default",
             "cast_frame_select_workspace_bytes", "cast_frame_select", "cast_diag_params_default",
             "cast_spectral_diagnostics_workspace_bytes", "cast_spectral_diagnostics",
-            "cast_phase_progress"]
+            "cast_phase_progress", "cast_rope_frequencies", "cast_rope", "cast_kv_append",
+            "cast_kv_read", "cast_kv_attn_workspace_bytes", "cast_kv_attn"]
 
 
 class CastError(RuntimeError):
@@ -67,8 +68,28 @@ class DiagParams(ctypes.Structure):
                 ("band_edges", ctypes.c_float * 9), ("eps", ctypes.c_float)]
 
 
+class RopeStruct(ctypes.Structure):
+    """cast_rope_params_t (include/cast.h)."""
+    _fields_ = [("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("n_axes", ctypes.c_int),
+                ("amplitude", ctypes.c_float), ("turns", ctypes.c_void_p), ("axis", ctypes.c_void_p)]
+
+
+class KvCacheStruct(ctypes.Structure):
+    """cast_kv_cache_t (include/cast.h)."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p), ("dtype", ctypes.c_int), ("pages", ctypes.c_int),
+                ("page", ctypes.c_int), ("H", ctypes.c_int), ("dh", ctypes.c_int)]
+
+
+class KvSeqsStruct(ctypes.Structure):
+    """cast_kv_seqs_t (include/cast.h)."""
+    _fields_ = [("cu", ctypes.c_void_p), ("len", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("n_seq", ctypes.c_int), ("n_tok", ctypes.c_int), ("max_pages", ctypes.c_int)]
+
+
 _lib = None
 _c = ctypes
+_ll = _c.c_longlong
 _vp, _i, _f, _sz = _c.c_void_p, _c.c_int, _c.c_float, _c.c_size_t
 
 
@@ -136,6 +157,20 @@ def load(path: str = LIB_PATH):
     lib.cast_phase_progress.restype = _i
     lib.cast_phase_progress.argtypes = [_vp, _c.POINTER(_i), _i, _i, _i, _i, _i,
                                         _c.POINTER(DiagParams), _vp, _vp]
+    lib.cast_rope_frequencies.restype = _i
+    lib.cast_rope_frequencies.argtypes = [_c.POINTER(_i), _i] + [_c.c_double, _i] + [_c.c_double] * 4 + [_vp, _vp]
+    lib.cast_rope.restype = _i
+    lib.cast_rope.argtypes = [_vp, _i, _i, _i, _i, _ll, _ll, _vp, _c.POINTER(RopeStruct), _i, _vp, _ll, _ll, _vp]
+    lib.cast_kv_append.restype = _i
+    lib.cast_kv_append.argtypes = [_c.POINTER(KvCacheStruct), _c.POINTER(KvSeqsStruct), _vp, _ll, _vp, _ll,
+                                   _c.POINTER(RopeStruct), _vp, _vp, _ll, _i, _vp, _vp]
+    lib.cast_kv_read.restype = _i
+    lib.cast_kv_read.argtypes = [_c.POINTER(KvCacheStruct), _vp, _i, _vp, _vp, _vp]
+    lib.cast_kv_attn_workspace_bytes.restype = _sz
+    lib.cast_kv_attn_workspace_bytes.argtypes = [_c.POINTER(KvCacheStruct), _c.POINTER(KvSeqsStruct), _i, _i, _i, _i, _i]
+    lib.cast_kv_attn.restype = _i
+    lib.cast_kv_attn.argtypes = [_vp, _ll, _i, _c.POINTER(KvCacheStruct), _c.POINTER(KvSeqsStruct), _i, _i, _i, _i,
+                                 _f, _vp, _vp, _vp, _sz, _vp]
     _lib = lib
     return lib
 
@@ -447,3 +482,306 @@ def par_debug_shapes(n_anchor, Hg, Wg, params: ParParams):
     """Shapes of the optional theta/gate ([pairs, tiles, bins]) and conf ([pairs, tiles])."""
     nt = -(-Hg // params.tile_h) * -(-Wg // params.tile_w)
     return (n_anchor - 1, nt, params.tile_h * (params.tile_w // 2 + 1)), (n_anchor - 1, nt)
+
+
+# ---------------------------------------------------------------------------
+# Cached history: rotary positions, paged append, page read, paged attention
+# ---------------------------------------------------------------------------
+
+ROPE_SCALING = {"none": 0, "linear": 1, "parts": 2}
+
+
+def _bad(msg: str):
+    raise CastError(2, msg)                        # CAST_ERR_SHAPE, before the library is asked
+
+
+def _want(name: str, t, dtypes, device=None, dense: bool = True):
+    """The binding's checks of a tensor the C ABI sees as a bare pointer."""
+    if t.dtype not in dtypes:
+        _bad(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if device is not None and t.device != device:
+        _bad(f"{name} is on {t.device}, expected {device}")
+    if dense and not t.is_contiguous():
+        _bad(f"{name} must be contiguous")
+    return t
+
+
+def _rows(name: str, t, heads, dh, n, device):
+    """Token stride of bf16 [n, heads, dh] with dense heads."""
+    import torch
+    _want(name, t, (torch.bfloat16,), device, dense=False)
+    if t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or t.shape[2] != dh:
+        _bad(f"{name} must be [{n}, {heads}, {dh}], got {list(t.shape)}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dh):
+        _bad(f"{name} must have dense heads")
+    return t.stride(0) if n > 1 else heads * dh
+
+
+def _on(device, stream):
+    """The stream's handle, after checking that `device` is current (kernels run there)."""
+    import torch
+    if device.type != "cuda":
+        _bad(f"tensors must be on a GPU, got {device}")
+    if device.index != torch.cuda.current_device():
+        _bad(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    return _stream(stream)
+
+
+def cast_rope_frequencies(axis_dims, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                          orig_len: float = 0.0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """Host tables of a rotation: (turns float64 [rot/2], axis uint8 [rot/2]), CPU tensors."""
+    import torch
+    lib = load()
+    dims = [int(d) for d in axis_dims]
+    if scaling not in ROPE_SCALING:
+        _bad(f"scaling must be one of {sorted(ROPE_SCALING)}, got {scaling!r}")
+    n = max(sum(max(d, 0) for d in dims) // 2, 1)
+    turns = torch.zeros(n, dtype=torch.float64)
+    axis = torch.zeros(n, dtype=torch.uint8)
+    arr = (ctypes.c_int * max(len(dims), 1))(*dims)
+    _check(lib.cast_rope_frequencies(arr, len(dims), base, ROPE_SCALING[scaling], factor, orig_len, beta_fast,
+                                     beta_slow, _ptr(turns), _ptr(axis)))
+    return turns, axis
+
+
+class RopeParams:
+    """cast_rope_params_t with its device tables (kept by a program once per model)."""
+
+    def __init__(self, turns, axis, n_axes: int = 1, interleaved: bool = False, amplitude: float = 1.0):
+        import torch
+        _want("turns", turns, (torch.float64,))
+        if turns.dim() != 1:
+            _bad("turns must have one dimension")
+        if axis is not None:
+            _want("axis", axis, (torch.uint8,), turns.device)
+            if axis.numel() != turns.numel():
+                _bad("axis must have one entry for each of turns")
+        self.turns, self.axis, self.n_axes, self.device = turns, axis, int(n_axes), turns.device
+        self.struct = RopeStruct(2 * turns.numel(), int(bool(interleaved)), int(n_axes), amplitude, _ptr(turns),
+                                 _ptr(axis))
+        self.ref = ctypes.byref(self.struct)
+
+
+def cast_rope_params_init(rot_dim: int, base: float = 10000.0, interleaved: bool = False, axes=None,
+                          scaling: str = "none", factor: float = 1.0, orig_len: float = 0.0,
+                          beta_fast: float = 32.0, beta_slow: float = 1.0, amplitude: float = 1.0,
+                          device=None) -> RopeParams:
+    """The rotation of the first rot_dim channels of a head, its tables on `device` (default:
+    the current one).  axes: channels of each position component (default: one component)."""
+    import torch
+    dims = [int(rot_dim)] if axes is None else [int(d) for d in axes]
+    if sum(dims) != rot_dim:
+        _bad(f"axes {dims} do not add up to rot_dim {rot_dim}")
+    turns, axis = cast_rope_frequencies(dims, base, scaling, factor, orig_len, beta_fast, beta_slow)
+    if device is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    return RopeParams(turns.to(device), axis.to(device), len(dims), interleaved, amplitude)
+
+
+def _pos(pos, n, rope, device):
+    import torch
+    _want("pos", pos, (torch.int32,), device)
+    if pos.numel() != n * rope.n_axes or pos.shape[0] != n:
+        _bad(f"pos must be [{n}, {rope.n_axes}], got {list(pos.shape)}")
+    return pos.data_ptr()
+
+
+def cast_rope(x, pos, rope: RopeParams, transpose: bool = False, out=None, stream=None):
+    """Rotary positions.  x [n, H, dh] fp32 or bf16 (device, any token and head strides); pos
+    int32 [n, n_axes] (or [n]).  `out` may be x itself.  transpose: turn the other way (the
+    gradient of the rotation).  Returns out."""
+    import torch
+    lib = load()
+    _want("x", x, (torch.float32, torch.bfloat16), dense=False)
+    if x.dim() != 3:
+        _bad(f"x must be [n, H, dh], got {list(x.shape)}")
+    n, H, dh = x.shape
+    if out is None:
+        out = torch.empty((n, H, dh), dtype=x.dtype, device=x.device)
+    _want("out", out, (x.dtype,), x.device, dense=False)
+    if out.shape != x.shape:
+        _bad(f"out must be {list(x.shape)}, got {list(out.shape)}")
+    if (x.stride(2) != 1 or out.stride(2) != 1) and n > 0:
+        _bad("the channels of x and out must be dense")
+    if rope.device != x.device:
+        _bad(f"the rotation's tables are on {rope.device}, x on {x.device}")
+    pp = _pos(pos, n, rope, x.device)
+    st = lambda t: (t.stride(0) if n > 1 else max(t.stride(0), H * dh), t.stride(1) if H > 1 else dh)  # noqa: E731
+    xs, os_ = st(x), st(out)
+    _check(lib.cast_rope(x.data_ptr(), 0 if x.dtype == torch.float32 else 1, n, H, dh, xs[0], xs[1], pp, rope.ref,
+                         int(bool(transpose)), out.data_ptr(), os_[0], os_[1], _on(x.device, stream)))
+    return out
+
+
+class KvCache:
+    """cast_kv_cache_t over tensors k, v [pages, page, H, dh]: bf16, or uint8 / float8_e4m3fn
+    codes with exponent bytes k_exp, v_exp uint8 [pages, H]."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        import torch
+        if k.dim() != 4 or v.shape != k.shape:
+            _bad(f"k and v must be [pages, page, H, dh] alike, got {list(k.shape)} and {list(v.shape)}")
+        codes = k.dtype != torch.bfloat16
+        _want("k", k, (torch.uint8, torch.float8_e4m3fn) if codes else (torch.bfloat16,))
+        _want("v", v, (k.dtype,), k.device)
+        self.k, self.v, self.k_exp, self.v_exp, self.device = k, v, k_exp, v_exp, k.device
+        self.pages, self.page, self.H, self.dh = k.shape
+        if codes:
+            for name, e in (("k_exp", k_exp), ("v_exp", v_exp)):
+                if e is None:
+                    _bad(f"an 8-bit cache needs {name}")
+                _want(name, e, (torch.uint8,), k.device)
+                if tuple(e.shape) != (self.pages, self.H):
+                    _bad(f"{name} must be [{self.pages}, {self.H}], got {list(e.shape)}")
+        elif k_exp is not None or v_exp is not None:
+            _bad("a bf16 cache has no exponents")
+        self.struct = KvCacheStruct(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), 2 if codes else 1, self.pages,
+                                    self.page, self.H, self.dh)
+        self.ref = ctypes.byref(self.struct)
+
+
+def cast_kv_cache_alloc(pages: int, page: int, H: int, dh: int, dtype=None, device=None) -> KvCache:
+    """A zeroed KvCache: dtype torch.bfloat16 (default) or torch.float8_e4m3fn."""
+    import torch
+    dtype = torch.bfloat16 if dtype is None else dtype
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    if dtype == torch.bfloat16:
+        mk = lambda: torch.zeros((pages, page, H, dh), dtype=dtype, device=device)  # noqa: E731
+        return KvCache(mk(), mk())
+    if dtype != torch.float8_e4m3fn:
+        _bad(f"a cache is bfloat16 or float8_e4m3fn, not {dtype}")
+    mk = lambda *s: torch.zeros(s, dtype=torch.uint8, device=device)  # noqa: E731
+    return KvCache(mk(pages, page, H, dh), mk(pages, page, H, dh), mk(pages, H), mk(pages, H))
+
+
+class KvSeqs:
+    """cast_kv_seqs_t over device int32 tensors cu [n_seq + 1], lens [n_seq] (WITH the call's
+    tokens) and table [n_seq, max_pages].  The tensors may be updated in place between calls;
+    the number of rows of a call is that of its tensors."""
+
+    def __init__(self, cu, lens, table):
+        import torch
+        for name, t in (("cu", cu), ("lens", lens), ("table", table)):
+            _want(name, t, (torch.int32,), cu.device)
+        if table.dim() != 2 or lens.shape != table.shape[:1] or tuple(cu.shape) != (table.shape[0] + 1,):
+            _bad(f"need cu [n_seq + 1], lens [n_seq], table [n_seq, max_pages], got {list(cu.shape)}, "
+                 f"{list(lens.shape)}, {list(table.shape)}")
+        self.cu, self.lens, self.table, self.device = cu, lens, table, cu.device
+        self._structs = {}
+
+    def ref(self, n_tok: int):
+        r = self._structs.get(n_tok)
+        if r is None:
+            s = KvSeqsStruct(_ptr(self.cu), _ptr(self.lens), _ptr(self.table), self.table.shape[0], n_tok,
+                             self.table.shape[1])
+            if len(self._structs) >= 64:
+                self._structs.clear()
+            r = self._structs[n_tok] = ctypes.byref(s)
+        return r
+
+
+def _same_device(cache, seqs):
+    if seqs.device != cache.device:
+        _bad(f"the sequences are on {seqs.device}, the cache on {cache.device}")
+
+
+def cast_kv_append(cache: KvCache, seqs: KvSeqs, k, v, rope: RopeParams | None = None, pos=None, q=None,
+                   q_out=None, stream=None):
+    """Store k, v (bf16 [n, H, dh], heads dense, any token stride) into the cache's pages, keys
+    rotated by `rope` (None: as they come) at pos (int32 [n, n_axes]; None: the token's index in
+    its sequence), and rotate the queries q [n, Hq, dh].  Returns q_out, or None without q."""
+    import torch
+    lib = load()
+    n, dev = k.shape[0], cache.device
+    _same_device(cache, seqs)
+    ks, vs = _rows("k", k, cache.H, cache.dh, n, dev), _rows("v", v, cache.H, cache.dh, n, dev)
+    qs, hq = 0, 0
+    if q is not None:
+        hq = q.shape[1] if q.dim() == 3 else 0
+        qs = _rows("q", q, hq, cache.dh, n, dev)
+        if q_out is None:
+            q_out = torch.empty((n, hq, cache.dh), dtype=q.dtype, device=dev)
+        _want("q_out", q_out, (torch.bfloat16,), dev)
+        if q_out.shape != q.shape:
+            _bad(f"q_out must be {list(q.shape)}, got {list(q_out.shape)}")
+    if rope is not None and rope.device != dev:
+        _bad(f"the rotation's tables are on {rope.device}, the cache on {dev}")
+    if rope is None and pos is not None:
+        _bad("pos is given without a rotation")
+    pp = None if pos is None else _pos(pos, n, rope, dev)
+    _check(lib.cast_kv_append(cache.ref, seqs.ref(n), k.data_ptr(), ks, v.data_ptr(), vs,
+                              None if rope is None else rope.ref, pp, _ptr(q), qs, hq,
+                              None if q is None else q_out.data_ptr(), _on(dev, stream)))
+    return None if q is None else q_out
+
+
+def cast_kv_read(cache: KvCache, pages, k_out=None, v_out=None, want_k: bool = True, want_v: bool = True,
+                 stream=None):
+    """The pages `pages` (int32 [m], device) as bf16 history blocks (k, v) [m, page, H, dh], the
+    layout of cast_route_kv and cast_anchor_attn; None where not wanted."""
+    import torch
+    lib = load()
+    _want("pages", pages, (torch.int32,), cache.device)
+    shape = (pages.numel(), cache.page, cache.H, cache.dh)
+    mk = lambda t, want: t if t is not None or not want else torch.empty(shape, dtype=torch.bfloat16, device=cache.device)  # noqa: E731
+    k_out, v_out = mk(k_out, want_k), mk(v_out, want_v)
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if t is not None:
+            _want(name, t, (torch.bfloat16,), cache.device)
+            if tuple(t.shape) != shape:
+                _bad(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    _check(lib.cast_kv_read(cache.ref, pages.data_ptr(), shape[0], _ptr(k_out), _ptr(v_out),
+                            _on(cache.device, stream)))
+    return k_out, v_out
+
+
+def _max_len(cache, seqs, max_len):
+    top = seqs.table.shape[1] * cache.page
+    return top if max_len is None else max(1, min(int(max_len), top))
+
+
+def cast_kv_attn_workspace_bytes(q, cache: KvCache, seqs: KvSeqs, max_len=None, causal: bool = True,
+                                 window: int = 0, sinks: int = 0) -> int:
+    return load().cast_kv_attn_workspace_bytes(cache.ref, seqs.ref(q.shape[0]), q.shape[1],
+                                               _max_len(cache, seqs, max_len), int(bool(causal)), window, sinks)
+
+
+def cast_kv_attn(q, cache: KvCache, seqs: KvSeqs, scale: float, causal: bool = True, window: int = 0,
+                 sinks: int = 0, max_len=None, out=None, lse_out=None, want_lse: bool = False, workspace=None,
+                 split: bool = True, stream=None):
+    """Attention of q (bf16 [n, Hq, dh], heads dense, any token stride) over the paged cache;
+    returns (out bf16 [n, Hq, dh], lse fp32 [n, Hq] or None).  max_len: the longest length
+    expected (default: what the table holds); split=True uses `workspace` (allocated here when
+    None) to cut long key ranges into pieces, split=False runs every row tile whole."""
+    import torch
+    lib = load()
+    if q.dim() != 3:
+        _bad(f"q must be [n, Hq, dh], got {list(q.shape)}")
+    n, hq, dev = q.shape[0], q.shape[1], cache.device
+    _same_device(cache, seqs)
+    qs = _rows("q", q, hq, cache.dh, n, dev)
+    if out is None:
+        out = torch.empty((n, hq, cache.dh), dtype=torch.bfloat16, device=dev)
+    else:
+        _want("out", out, (torch.bfloat16,), dev)
+        if out.shape != q.shape:
+            _bad(f"out must be {list(q.shape)}, got {list(out.shape)}")
+    if lse_out is None:
+        if want_lse:
+            lse_out = torch.empty((n, hq), dtype=torch.float32, device=dev)
+    else:
+        _want("lse_out", lse_out, (torch.float32,), dev)
+        if tuple(lse_out.shape) != (n, hq):
+            _bad(f"lse_out must be {[n, hq]}, got {list(lse_out.shape)}")
+    top, sref, causal = _max_len(cache, seqs, max_len), seqs.ref(n), int(bool(causal))
+    strm = _on(dev, stream)
+    ws, wsb = None, 0
+    if split:
+        if workspace is not None:
+            _want("workspace", workspace, (workspace.dtype,), dev)
+            ws, wsb = workspace, workspace.numel() * workspace.element_size()
+        else:
+            ws, wsb = _ws(lib.cast_kv_attn_workspace_bytes(cache.ref, sref, hq, top, causal, window, sinks), dev, None)
+    _check(lib.cast_kv_attn(q.data_ptr(), qs, hq, cache.ref, sref, top, causal, window, sinks, scale, out.data_ptr(),
+                            _ptr(lse_out), _ptr(ws), wsb, strm))
+    return out, lse_out

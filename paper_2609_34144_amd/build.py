@@ -36,6 +36,8 @@ UNITS = [("par.hip", "par", ["-fno-signed-zeros"])] + [
     # MFMA accumulators in VGPRs: the softmax reads S directly, and the Q operands
     # are parked in AGPRs by the kernel itself
     ("anchor_attn.hip", "anchor_attn", ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]),
+    ("kv_attn.hip", "kv_attn", ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]),
+    ("kv_cache.hip", "kv_cache", []),
     ("route_kv.hip", "route_kv", []),
     ("route_coupled.hip", "route_coupled", []),
     ("frame_select.hip", "frame_select", []),

@@ -2,10 +2,12 @@
 // dispatch to the kernel launchers.  Every entry point validates all of its
 // arguments before anything is enqueued and reports failures as a status plus
 // a thread-local detail string.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "cast_common.h"
@@ -523,6 +525,250 @@ cast_status_t cast_phase_progress(const float* ref, const int* anchors, int n_an
   if (!aligned(ref, 4) || !aligned(p_out, 4)) return fail(CAST_ERR_SHAPE, "progress: misaligned buffers");
   return launch_phase_progress(ref, anchors, n_anchor, Hg, Wg, D, params->tile_h, params->tile_w,
                                p_out, stream);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Cached history: rotation, paged append, page read, paged attention
+// ---------------------------------------------------------------------------
+static cast_status_t rope_check(const cast_rope_params_t* p, int dh, const char* who) {
+  if (p->rot_dim < 2 || p->rot_dim > dh || p->rot_dim % 2 != 0)
+    return fail(CAST_ERR_SHAPE, "%s: rot_dim must be even and in [2, dh] (got %d)", who, p->rot_dim);
+  if (p->interleaved != 0 && p->interleaved != 1) return fail(CAST_ERR_SHAPE, "%s: interleaved must be 0 or 1", who);
+  if (p->n_axes < 1 || p->n_axes > 3) return fail(CAST_ERR_SHAPE, "%s: n_axes must be in [1, 3]", who);
+  if (!(p->amplitude >= -3.0e38f && p->amplitude <= 3.0e38f))
+    return fail(CAST_ERR_SHAPE, "%s: amplitude must be finite", who);
+  if (p->turns == nullptr) return fail(CAST_ERR_NULL, "%s: the rotation's turns are NULL", who);
+  if (!aligned(p->turns, 8)) return fail(CAST_ERR_SHAPE, "%s: the rotation's turns must be 8-byte aligned", who);
+  return CAST_OK;
+}
+
+extern "C" {
+
+cast_status_t cast_rope_frequencies(const int* axis_dims, int n_axes, double base, int scaling,
+                                    double factor, double orig_len, double beta_fast,
+                                    double beta_slow, double* turns_out, uint8_t* axis_out) {
+  if (axis_dims == nullptr || turns_out == nullptr || axis_out == nullptr)
+    return fail(CAST_ERR_NULL, "rope: axis_dims, turns_out and axis_out are required");
+  if (n_axes < 1 || n_axes > 3) return fail(CAST_ERR_SHAPE, "rope: n_axes must be in [1, 3]");
+  long long sum = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    if (axis_dims[a] < 2 || axis_dims[a] % 2 != 0)
+      return fail(CAST_ERR_SHAPE, "rope: axis %d has %d channels, need an even number >= 2", a, axis_dims[a]);
+    sum += axis_dims[a];
+  }
+  if (sum > kRopeMaxDim) return fail(CAST_ERR_SHAPE, "rope: %lld rotated channels exceed %d", sum, kRopeMaxDim);
+  if (!(base > 0.0) || !(base < 1e300)) return fail(CAST_ERR_SHAPE, "rope: base must be finite and > 0");
+  if (scaling < CAST_ROPE_SCALE_NONE || scaling > CAST_ROPE_SCALE_PARTS)
+    return fail(CAST_ERR_SHAPE, "rope: unknown scaling %d", scaling);
+  if (scaling != CAST_ROPE_SCALE_NONE && (!(factor >= 1.0) || !(factor < 1e300)))
+    return fail(CAST_ERR_SHAPE, "rope: factor must be finite and >= 1");
+  if (scaling == CAST_ROPE_SCALE_PARTS &&
+      (!(orig_len > 0.0) || !(orig_len < 1e300) || !(beta_slow >= 0.0) || !(beta_fast > beta_slow) || !(beta_fast < 1e300)))
+    return fail(CAST_ERR_SHAPE, "rope: scaling by parts needs orig_len > 0 and beta_fast > beta_slow >= 0");
+  int j = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    for (int i = 0; i < axis_dims[a] / 2; ++i, ++j) {
+      double t = pow(base, -2.0 * i / axis_dims[a]) / 6.283185307179586476925286766559;
+      if (scaling == CAST_ROPE_SCALE_LINEAR) {
+        t /= factor;
+      } else if (scaling == CAST_ROPE_SCALE_PARTS) {
+        double g = (orig_len * t - beta_slow) / (beta_fast - beta_slow);
+        g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
+        t *= g + (1.0 - g) / factor;
+      }
+      turns_out[j] = t;
+      axis_out[j] = (uint8_t)a;
+    }
+  }
+  return CAST_OK;
+}
+
+cast_status_t cast_rope(const void* x, int dtype, int n, int H, int dh, long long x_token_stride,
+                        long long x_head_stride, const int32_t* pos,
+                        const cast_rope_params_t* params, int transpose, void* out,
+                        long long out_token_stride, long long out_head_stride,
+                        hipStream_t stream) {
+  if (params == nullptr) return fail(CAST_ERR_NULL, "rope: params is NULL");
+  if (n < 0 || H < 1) return fail(CAST_ERR_SHAPE, "rope: need n >= 0 and H >= 1 (got %d %d)", n, H);
+  if (!dh_ok(dh)) return fail(CAST_ERR_UNSUPPORTED, "rope: dh must be 32, 64 or 128 (got %d)", dh);
+  if (dtype != 0 && dtype != 1) return fail(CAST_ERR_SHAPE, "rope: dtype must be 0 (fp32) or 1 (bf16)");
+  if (transpose != 0 && transpose != 1) return fail(CAST_ERR_SHAPE, "rope: transpose must be 0 or 1");
+  if ((long long)n * H >= (1LL << 33)) return fail(CAST_ERR_UNSUPPORTED, "rope: n * H * dh must stay below 2^40");
+  const long long top = 1LL << 40;
+  if (x_token_stride < dh || x_head_stride < dh || out_token_stride < dh || out_head_stride < dh ||
+      x_token_stride > top || x_head_stride > top || out_token_stride > top || out_head_stride > top)
+    return fail(CAST_ERR_SHAPE, "rope: strides must be in [dh, 2^40]");
+  // two elements of out must not share an address: one stride steps over the whole other extent
+  if (n > 1 && H > 1 && out_token_stride < (H - 1) * out_head_stride + dh && out_head_stride < (n - 1) * out_token_stride + dh)
+    return fail(CAST_ERR_SHAPE, "rope: tokens and heads of out overlap");
+  cast_status_t st = rope_check(params, dh, "rope");
+  if (st != CAST_OK) return st;
+  if (n == 0) return CAST_OK;
+  if (x == nullptr || pos == nullptr || out == nullptr) return fail(CAST_ERR_NULL, "rope: x, pos and out are required");
+  const size_t esz = dtype == 0 ? 4 : 2;
+  if (!aligned(x, esz) || !aligned(out, esz) || !aligned(pos, 4)) return fail(CAST_ERR_SHAPE, "rope: misaligned buffers");
+  if (x == out && (x_token_stride != out_token_stride || x_head_stride != out_head_stride))
+    return fail(CAST_ERR_SHAPE, "rope: out is x with other strides");
+  const long long e16 = 16 / (long long)esz;
+  const bool wide = aligned(x, 16) && aligned(out, 16) && x_token_stride % e16 == 0 && x_head_stride % e16 == 0 &&
+                    out_token_stride % e16 == 0 && out_head_stride % e16 == 0;
+  return launch_rope(x, dtype, n, H, dh, x_token_stride, x_head_stride, pos, *params, transpose, out,
+                     out_token_stride, out_head_stride, wide, stream);
+}
+
+}  // extern "C"
+
+static cast_status_t cache_sizes(const cast_kv_cache_t* c, const char* who) {
+  if (c == nullptr) return fail(CAST_ERR_NULL, "%s: cache is NULL", who);
+  if (c->dtype != 1 && c->dtype != 2) return fail(CAST_ERR_SHAPE, "%s: cache dtype must be 1 (bf16) or 2 (e4m3)", who);
+  if (!dh_ok(c->dh)) return fail(CAST_ERR_UNSUPPORTED, "%s: dh must be 32, 64 or 128 (got %d)", who, c->dh);
+  if (c->pages < 1 || c->page < 1 || c->H < 1)
+    return fail(CAST_ERR_SHAPE, "%s: need pages, page, H >= 1 (got %d %d %d)", who, c->pages, c->page, c->H);
+  if ((long long)c->pages * c->page >= (1LL << 31))
+    return fail(CAST_ERR_UNSUPPORTED, "%s: pages * page must stay below 2^31", who);
+  if (c->H > 4096 || c->page >= (1 << 24) || (long long)c->page * c->H * c->H >= (1LL << 40))
+    return fail(CAST_ERR_UNSUPPORTED, "%s: H must be at most 4096, page below 2^24 and page * H * H below 2^40", who);
+  return CAST_OK;
+}
+
+static cast_status_t cache_pointers(const cast_kv_cache_t* c, const char* who) {
+  if (c->k == nullptr || c->v == nullptr) return fail(CAST_ERR_NULL, "%s: the cache's k and v are required", who);
+  if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(CAST_ERR_SHAPE, "%s: the cache must be 16-byte aligned", who);
+  if (c->dtype == 2 && (c->k_exp == nullptr || c->v_exp == nullptr))
+    return fail(CAST_ERR_NULL, "%s: an e4m3 cache needs k_exp and v_exp", who);
+  return CAST_OK;
+}
+
+static cast_status_t seqs_sizes(const cast_kv_seqs_t* s, int page, const char* who) {
+  if (s == nullptr) return fail(CAST_ERR_NULL, "%s: seqs is NULL", who);
+  if (s->n_seq < 1 || s->n_tok < 0 || s->max_pages < 1)
+    return fail(CAST_ERR_SHAPE, "%s: need n_seq, max_pages >= 1 and n_tok >= 0 (got %d %d %d)", who, s->n_seq, s->max_pages, s->n_tok);
+  if (s->n_seq > (1 << 20) || s->n_tok >= (1 << 30) || s->max_pages >= (1 << 24) ||
+      (long long)s->max_pages * page >= (1LL << 30) || (long long)s->max_pages * page * page >= (1LL << 40) ||
+      (long long)s->n_tok * page >= (1LL << 40) || s->n_tok >= (1LL << 24) * page)
+    return fail(CAST_ERR_UNSUPPORTED, "%s: more sequences (2^20), rows or pages than the indexing takes", who);
+  return CAST_OK;
+}
+
+static cast_status_t seqs_pointers(const cast_kv_seqs_t* s, const char* who) {
+  if (s->cu == nullptr || s->len == nullptr || s->table == nullptr)
+    return fail(CAST_ERR_NULL, "%s: cu, len and table are required", who);
+  if (!aligned(s->cu, 4) || !aligned(s->len, 4) || !aligned(s->table, 4))
+    return fail(CAST_ERR_SHAPE, "%s: cu, len and table must be 4-byte aligned", who);
+  return CAST_OK;
+}
+
+// rows of `heads` dense heads of dh, `stride` elements apart
+static cast_status_t rows_check(const void* p, long long stride, int heads, int dh, const char* who, const char* what) {
+  if (p == nullptr) return fail(CAST_ERR_NULL, "%s: %s is NULL", who, what);
+  if (!aligned(p, 16)) return fail(CAST_ERR_SHAPE, "%s: %s must be 16-byte aligned", who, what);
+  if (stride < (long long)heads * dh || stride % 8 != 0 || stride > (1LL << 32))
+    return fail(CAST_ERR_SHAPE, "%s: the token stride of %s must be a multiple of 8 in [%lld, 2^32]", who, what, (long long)heads * dh);
+  return CAST_OK;
+}
+
+extern "C" {
+
+cast_status_t cast_kv_append(const cast_kv_cache_t* cache, const cast_kv_seqs_t* seqs,
+                             const void* k, long long k_stride, const void* v, long long v_stride,
+                             const cast_rope_params_t* rope, const int32_t* pos,
+                             const void* q, long long q_stride, int Hq, void* q_out,
+                             hipStream_t stream) {
+  cast_status_t st = cache_sizes(cache, "kv_append");
+  if (st == CAST_OK) st = seqs_sizes(seqs, cache->page, "kv_append");
+  if (st == CAST_OK && rope != nullptr) st = rope_check(rope, cache->dh, "kv_append");
+  if (st != CAST_OK) return st;
+  if (rope != nullptr && pos == nullptr && rope->n_axes != 1)
+    return fail(CAST_ERR_NULL, "kv_append: a rotation of %d axes needs pos", rope->n_axes);
+  if (rope != nullptr && !aligned(pos, 4)) return fail(CAST_ERR_SHAPE, "kv_append: pos must be 4-byte aligned");
+  if (q != nullptr && rope == nullptr) return fail(CAST_ERR_NULL, "kv_append: q is rotated, but rope is NULL");
+  if (q != nullptr && (Hq < 1 || Hq > (1 << 16))) return fail(CAST_ERR_SHAPE, "kv_append: need 1 <= Hq <= 65536 (got %d)", Hq);
+  if (seqs->n_tok == 0) return CAST_OK;
+  st = cache_pointers(cache, "kv_append");
+  if (st == CAST_OK) st = seqs_pointers(seqs, "kv_append");
+  if (st == CAST_OK) st = rows_check(k, k_stride, cache->H, cache->dh, "kv_append", "k");
+  if (st == CAST_OK) st = rows_check(v, v_stride, cache->H, cache->dh, "kv_append", "v");
+  if (st == CAST_OK && q != nullptr) st = rows_check(q, q_stride, Hq, cache->dh, "kv_append", "q");
+  if (st == CAST_OK && q != nullptr) st = rows_check(q_out, (long long)Hq * cache->dh, Hq, cache->dh, "kv_append", "q_out");
+  if (st != CAST_OK) return st;
+  if (q != nullptr && q == q_out && q_stride != (long long)Hq * cache->dh)
+    return fail(CAST_ERR_SHAPE, "kv_append: q_out is q with another stride");
+  return launch_kv_append(*cache, *seqs, k, k_stride, v, v_stride, rope, pos, q, q_stride, Hq, q_out, stream);
+}
+
+cast_status_t cast_kv_read(const cast_kv_cache_t* cache, const int32_t* page_idx, int m,
+                           void* k_out, void* v_out, hipStream_t stream) {
+  cast_status_t st = cache_sizes(cache, "kv_read");
+  if (st != CAST_OK) return st;
+  if (m < 0) return fail(CAST_ERR_SHAPE, "kv_read: m must be >= 0 (got %d)", m);
+  if (m == 0) return CAST_OK;
+  st = cache_pointers(cache, "kv_read");
+  if (st != CAST_OK) return st;
+  if (page_idx == nullptr || (k_out == nullptr && v_out == nullptr))
+    return fail(CAST_ERR_NULL, "kv_read: page_idx and one of k_out, v_out are required");
+  if (!aligned(page_idx, 4) || !aligned(k_out, 16) || !aligned(v_out, 16))
+    return fail(CAST_ERR_SHAPE, "kv_read: page_idx must be 4-byte, k_out and v_out 16-byte aligned");
+  return launch_kv_read(*cache, page_idx, m, k_out, v_out, stream);
+}
+
+}  // extern "C"
+
+static cast_status_t kv_attn_sizes(const cast_kv_cache_t* cache, const cast_kv_seqs_t* seqs, int Hq, int max_len,
+                                   int causal, int window, int sinks) {
+  cast_status_t st = cache_sizes(cache, "kv_attn");
+  if (st == CAST_OK) st = seqs_sizes(seqs, cache->page, "kv_attn");
+  if (st != CAST_OK) return st;
+  if (Hq < 1 || Hq > (1 << 16) || Hq % cache->H != 0)
+    return fail(CAST_ERR_SHAPE, "kv_attn: Hq must be a multiple of the cache's %d heads, at most 65536 (got %d)", cache->H, Hq);
+  if ((long long)seqs->n_tok * Hq >= (1LL << 31))
+    return fail(CAST_ERR_UNSUPPORTED, "kv_attn: n_tok * Hq must stay below 2^31");
+  if (max_len < 1) return fail(CAST_ERR_SHAPE, "kv_attn: max_len must be >= 1 (got %d)", max_len);
+  if (causal != 0 && causal != 1) return fail(CAST_ERR_SHAPE, "kv_attn: causal must be 0 or 1");
+  if (window < 0 || sinks < 0) return fail(CAST_ERR_SHAPE, "kv_attn: window and sinks must be >= 0");
+  return CAST_OK;
+}
+
+static KvAttnPlan make_kv_attn_plan(const cast_kv_cache_t* c, const cast_kv_seqs_t* s, int Hq, int max_len,
+                                    int window, int sinks) {
+  return kv_attn_plan(s->n_tok, s->n_seq, Hq / c->H, c->H, c->dh, std::min<long long>(max_len, (long long)s->max_pages * c->page),
+                      std::min(window, 1 << 30), sinks, device_cu_count());
+}
+
+extern "C" {
+
+size_t cast_kv_attn_workspace_bytes(const cast_kv_cache_t* cache, const cast_kv_seqs_t* seqs,
+                                    int Hq, int max_len, int causal, int window, int sinks) {
+  if (kv_attn_sizes(cache, seqs, Hq, max_len, causal, window, sinks) != CAST_OK) return 0;
+  return make_kv_attn_plan(cache, seqs, Hq, max_len, window, sinks).bytes;
+}
+
+cast_status_t cast_kv_attn(const void* q, long long q_stride, int Hq, const cast_kv_cache_t* cache,
+                           const cast_kv_seqs_t* seqs, int max_len, int causal, int window,
+                           int sinks, float scale, void* out, float* lse_out, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream) {
+  cast_status_t st = kv_attn_sizes(cache, seqs, Hq, max_len, causal, window, sinks);
+  if (st != CAST_OK) return st;
+  if (!(scale > 0.0f) || scale > 3.0e38f) return fail(CAST_ERR_SHAPE, "kv_attn: scale must be finite and > 0");
+  if (seqs->n_tok == 0) return CAST_OK;
+  st = cache_pointers(cache, "kv_attn");
+  if (st == CAST_OK) st = seqs_pointers(seqs, "kv_attn");
+  if (st == CAST_OK) st = rows_check(q, q_stride, Hq, cache->dh, "kv_attn", "q");
+  if (st == CAST_OK) st = rows_check(out, (long long)Hq * cache->dh, Hq, cache->dh, "kv_attn", "out");
+  if (st != CAST_OK) return st;
+  if (!aligned(lse_out, 4)) return fail(CAST_ERR_SHAPE, "kv_attn: lse_out must be 4-byte aligned");
+  KvAttnPlan plan = make_kv_attn_plan(cache, seqs, Hq, max_len, window, sinks);
+  if (workspace == nullptr) {
+    plan.pieces = 1;                               // every row tile whole
+  } else {
+    if (!aligned(workspace, kWsAlign))
+      return fail(CAST_ERR_WORKSPACE, "kv_attn: workspace must be %zu-byte aligned", kWsAlign);
+    if (plan.pieces > 1 && workspace_bytes < plan.bytes)
+      return fail(CAST_ERR_WORKSPACE, "kv_attn: workspace has %zu bytes, %zu needed", workspace_bytes, plan.bytes);
+  }
+  return launch_kv_attn(q, q_stride, Hq, *cache, *seqs, causal, std::min(window, 1 << 30), sinks, scale, out, lse_out,
+                        plan, workspace, stream);
 }
 
 }  // extern "C"

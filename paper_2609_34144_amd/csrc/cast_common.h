@@ -146,4 +146,35 @@ cast_status_t launch_phase_progress(const float* ref, const int* anchors, int n_
                                     int Wg, int D, int tile_h, int tile_w, float* p_out,
                                     hipStream_t stream);
 
+// ---------------------------------------------------------------------------
+// Cached history: rotation, paged append, page read, paged attention
+// ---------------------------------------------------------------------------
+constexpr int kRopeMaxDim = 128;
+// `wide`: buffers and strides 16-byte aligned
+cast_status_t launch_rope(const void* x, int dtype, int n, int H, int dh, long long xt, long long xh,
+                          const int32_t* pos, const cast_rope_params_t& p, int transpose, void* out,
+                          long long yt, long long yh, bool wide, hipStream_t stream);
+cast_status_t launch_kv_append(const cast_kv_cache_t& c, const cast_kv_seqs_t& s, const void* k, long long ks,
+                               const void* v, long long vs, const cast_rope_params_t* rope, const int32_t* pos,
+                               const void* q, long long qs, int Hq, void* q_out, hipStream_t stream);
+cast_status_t launch_kv_read(const cast_kv_cache_t& c, const int32_t* idx, int m, void* ko, void* vo,
+                             hipStream_t stream);
+
+struct KvSeqs;
+KvSeqs make_seqs(const cast_kv_seqs_t& s, int page);
+
+// How a call of cast_kv_attn is cut up.  `bytes` of workspace hold this plan and that of any
+// smaller max_len.
+struct KvAttnPlan {
+  bool few_rows;                 // 32-row workgroups (else 128)
+  int row_tiles;                 // upper bound over all ways to share the rows out
+  int pieces, piece_tiles;       // pieces along the keys, key tiles of each
+  size_t part_bytes, bytes;
+};
+KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, long long max_len, int window,
+                        int sinks, int cus);
+cast_status_t launch_kv_attn(const void* q, long long q_stride, int Hq, const cast_kv_cache_t& c,
+                             const cast_kv_seqs_t& s, int causal, int window, int sinks, float scale, void* out,
+                             float* lse, const KvAttnPlan& plan, void* workspace, hipStream_t stream);
+
 }  // namespace cast

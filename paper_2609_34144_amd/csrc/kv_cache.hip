@@ -1,0 +1,610 @@
+// Rotary positions, appending to a paged cache with the rotation on the way, and reading
+// pages back as bf16 blocks.  All three are bound by HBM (or, for a few tokens, by the
+// latency of one launch): every value is read once, converted in registers, written once.
+#include <algorithm>
+
+#include "kv_device.h"
+
+namespace cast {
+
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256;
+constexpr int kTok = 4;          // tokens per block of the rotating kernels: 4 x 64 pairs = one angle a thread
+constexpr int kMaxPairs = 64;
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+__device__ __forceinline__ float to_f32(uint16_t w) { return __uint_as_float((uint32_t)w << 16); }
+__device__ __forceinline__ float to_f32(float w) { return w; }
+__device__ __forceinline__ void from_f32(uint16_t* p, float v) { *p = (uint16_t)pack_bf16(v, 0.0f); }
+__device__ __forceinline__ void from_f32(float* p, float v) { *p = v; }
+
+// eight consecutive channels
+__device__ __forceinline__ void load8(const uint16_t* p, float* f) {
+  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = bf16lo(w[i]);
+    f[2 * i + 1] = bf16hi(w[i]);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, float* f) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[i] = a[i];
+    f[4 + i] = b[i];
+  }
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float* f) {
+  *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float* f) {
+  *reinterpret_cast<f32x4*>(p) = f32x4{f[0], f[1], f[2], f[3]};
+  *reinterpret_cast<f32x4*>(p + 4) = f32x4{f[4], f[5], f[6], f[7]};
+}
+
+// How the channels of a head are shared out over threads ("items"), each with both
+// channels of its pairs, so that out may be x itself:
+//   2  half layout, rot a multiple of 16: item i < rot/16 takes chunks i and i + rot/16 of
+//      eight channels, the others a chunk of the channels that pass through
+//   1  interleaved layout, rot a multiple of 8: item i takes chunk i
+//   0  any rot, any alignment: item j < rot/2 takes pair j, the others one channel
+struct Items {
+  int mode, per_head;
+  FastDiv div;                   // by per_head
+};
+Items plan_items(int rot, int inter, int dh, bool wide) {
+  Items t;
+  t.mode = wide && !inter && rot % 16 == 0 ? 2 : wide && (inter || rot == 0) && rot % 8 == 0 ? 1 : 0;
+  t.per_head = t.mode == 2 ? rot / 16 + (dh - rot) / 8 : t.mode == 1 ? dh / 8 : rot / 2 + (dh - rot);
+  t.div = fast_div(t.per_head);
+  return t;
+}
+
+// cs[j] = (cos, sin) of pair j, x and y the same head's row in and out
+template <class T>
+__device__ __forceinline__ void rotate_item(const T* x, T* y, int i, int mode, int rot, int inter,
+                                            const f32x2* cs) {
+  if (mode == 2) {
+    const int half = rot >> 1;
+    if (i < (rot >> 4)) {
+      float a[8], b[8], p[8], q[8];
+      load8(x + 8 * i, a);
+      load8(x + 8 * i + half, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const f32x2 c = cs[8 * i + e];
+        p[e] = fmaf(a[e], c.x, -(b[e] * c.y));
+        q[e] = fmaf(a[e], c.y, b[e] * c.x);
+      }
+      store8(y + 8 * i, p);
+      store8(y + 8 * i + half, q);
+      return;
+    }
+    const int c = rot + 8 * (i - (rot >> 4));
+    float a[8];
+    load8(x + c, a);
+    store8(y + c, a);
+  } else if (mode == 1) {
+    float a[8];
+    load8(x + 8 * i, a);
+    if (8 * i < rot) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x2 c = cs[4 * i + e];
+        const float u = a[2 * e], w = a[2 * e + 1];
+        a[2 * e] = fmaf(u, c.x, -(w * c.y));
+        a[2 * e + 1] = fmaf(u, c.y, w * c.x);
+      }
+    }
+    store8(y + 8 * i, a);
+  } else if (i < (rot >> 1)) {
+    const int c0 = inter ? 2 * i : i, c1 = inter ? 2 * i + 1 : i + (rot >> 1);
+    const f32x2 c = cs[i];
+    const float u = to_f32(x[c0]), w = to_f32(x[c1]);
+    from_f32(y + c0, fmaf(u, c.x, -(w * c.y)));
+    from_f32(y + c1, fmaf(u, c.y, w * c.x));
+  } else {
+    const int c = rot + (i - (rot >> 1));
+    y[c] = x[c];
+  }
+}
+
+// (cos, sin) of the block's tokens' pairs into LDS: token of the block tt, position of axis
+// a given by pos_of(tt, a).  sincospif on the reduced angle: full fp32 precision.
+template <class F>
+__device__ __forceinline__ void fill_angles(f32x2 (*cs)[kMaxPairs], const Rope& r, F&& pos_of) {
+  const int pairs = r.rot >> 1;
+  for (int t = threadIdx.x; t < kTok * kMaxPairs; t += kThreads) {
+    const int tt = t / kMaxPairs, j = t % kMaxPairs;
+    if (j < pairs) {
+      float s, c;
+      sincospif(2.0f * rope_revs(r.turns[j], pos_of(tt, rope_axis(r, j))), &s, &c);
+      cs[tt][j] = f32x2{c * r.amp, s * r.amp * r.sign};
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// cast_rope
+// ---------------------------------------------------------------------------
+// One block takes kTok tokens and one of gridDim.y shares of the heads; the angles of a
+// token are formed once per block and shared by its heads.  Few tokens: the heads are
+// shared out over more blocks (latency); many: one block takes them all.
+template <class T>
+__global__ __launch_bounds__(kThreads) void rope_kernel(const T* x, long long xt, long long xh, T* y,
+                                                        long long yt, long long yh, int n, int H,
+                                                        int heads, Rope r, Items it) {
+  __shared__ f32x2 cs[kTok][kMaxPairs];
+  const int t0 = blockIdx.x * kTok, nt = min(kTok, n - t0);
+  fill_angles(cs, r, [&](int tt, int a) { return r.pos[(long long)min(t0 + tt, n - 1) * r.n_axes + a]; });
+  __syncthreads();
+  const int h0 = blockIdx.y * heads, nh = min(heads, H - h0);
+  const int per_tok = nh * it.per_head;
+#pragma unroll 2
+  for (int i = threadIdx.x; i < nt * per_tok; i += kThreads) {
+    const int tt = i / per_tok, rem = i - tt * per_tok;
+    const int h = div_by(rem, it.div), item = rem - h * it.per_head;
+    const long long t = t0 + tt;
+    rotate_item(x + t * xt + (h0 + h) * xh, y + t * yt + (h0 + h) * yh, item, it.mode, r.rot, r.inter, cs[tt]);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// cast_kv_append, bf16 cache (and the queries of both)
+// ---------------------------------------------------------------------------
+struct AppendArgs {
+  KvSeqs s;
+  Rope r;
+  Items it;                      // rotation of one head
+  const uint16_t* k;
+  const uint16_t* v;
+  const uint16_t* q;
+  uint16_t* q_out;
+  void* kc;
+  void* vc;
+  uint8_t* ke;
+  uint8_t* ve;
+  long long ks, vs, qs;          // token strides
+  int H, Hq, dh, pages, page;
+  int heads;                     // heads of K, V and Q together per block
+  int q_blocks_x, q_shares;      // 8-bit: blocks of the queries in front of the pages'
+};
+
+// Sequence, index in it and row of the cache (-1: none) of a call's row: one wave per row.
+__device__ __forceinline__ void locate(const AppendArgs& a, int row, int* index, int* slot, int* mine) {
+  const int b = find_seq(a.s.n_seq, row, [&](int i) { return seq_row(a.s, i); });
+  const int beg = seq_row(a.s, b), end = seq_row(a.s, b + 1);
+  const int t = seq_len(a.s, b) - (end - row);
+  const bool in = row >= beg && row < end;
+  int at = -1;
+  if (in && t >= 0) {
+    const int p = div_by(t, a.s.page);
+    const int id = a.s.table[(long long)b * a.s.max_pages + p];
+    if (id >= 0 && id < a.pages) at = id * a.page + (t - p * a.page);
+  }
+  *index = t;
+  *slot = at;
+  *mine = in;
+}
+
+// Heads are counted K 0 .. H, V .. 2 H, Q .. 2 H + Hq; block (x, y) takes kTok tokens and
+// the heads [y heads, (y + 1) heads) of that count, from `first` on.
+__device__ __forceinline__ void append_rows(const AppendArgs& a, int bx, int by, int first,
+                                            f32x2 (*cs)[kMaxPairs], int* index, int* slot, int* mine) {
+  const int t0 = bx * kTok, n = a.s.n_tok, nt = min(kTok, n - t0);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave < nt) locate(a, t0 + wave, index + wave, slot + wave, mine + wave);
+  __syncthreads();
+  if (a.r.rot > 0) {
+    fill_angles(cs, a.r, [&](int tt, int ax) {
+      const int t = min(tt, nt - 1);
+      return a.r.pos != nullptr ? a.r.pos[(long long)(t0 + t) * a.r.n_axes + ax] : index[t];
+    });
+    __syncthreads();
+  }
+  const int h0 = first + by * a.heads, nh = min(a.heads, 2 * a.H + a.Hq - h0);
+  const int per_tok = nh * a.it.per_head;
+  const long long row = (long long)a.H * a.dh;
+  for (int i = threadIdx.x; i < nt * per_tok; i += kThreads) {
+    const int tt = i / per_tok, rem = i - tt * per_tok;
+    int h = div_by(rem, a.it.div);
+    const int item = rem - h * a.it.per_head;
+    h += h0;
+    const long long t = t0 + tt;
+    if (h < 2 * a.H) {
+      if (slot[tt] < 0) continue;
+      const bool is_v = h >= a.H;
+      if (is_v) h -= a.H;
+      const uint16_t* x = is_v ? a.v + t * a.vs + h * a.dh : a.k + t * a.ks + h * a.dh;
+      uint16_t* y = static_cast<uint16_t*>(is_v ? a.vc : a.kc) + (long long)slot[tt] * row + h * a.dh;
+      if (is_v) {
+        // the items of a head cover its channels in some order: copy the same ones
+        if (a.it.mode == 2) {
+          const bool two = item < (a.r.rot >> 4);
+          const int c = two ? 8 * item : a.r.rot + 8 * (item - (a.r.rot >> 4));
+          const u32x4 w = *reinterpret_cast<const u32x4*>(x + c);
+          if (two) {
+            const u32x4 w2 = *reinterpret_cast<const u32x4*>(x + c + (a.r.rot >> 1));
+            *reinterpret_cast<u32x4*>(y + c + (a.r.rot >> 1)) = w2;
+          }
+          *reinterpret_cast<u32x4*>(y + c) = w;
+        } else if (a.it.mode == 1) {
+          *reinterpret_cast<u32x4*>(y + 8 * item) = *reinterpret_cast<const u32x4*>(x + 8 * item);
+        } else if (item < a.dh / 8) {
+          *reinterpret_cast<u32x4*>(y + 8 * item) = *reinterpret_cast<const u32x4*>(x + 8 * item);
+        }
+      } else {
+        rotate_item(x, y, item, a.it.mode, a.r.rot, a.r.inter, cs[tt]);
+      }
+    } else if (mine[tt]) {
+      h -= 2 * a.H;
+      rotate_item(a.q + t * a.qs + h * a.dh, a.q_out + (t * a.Hq + h) * a.dh, item, a.it.mode, a.r.rot, a.r.inter, cs[tt]);
+    }
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
+  __shared__ f32x2 cs[kTok][kMaxPairs];
+  __shared__ int index[kTok], slot[kTok], mine[kTok];
+  append_rows(a, blockIdx.x, blockIdx.y, 0, cs, index, slot, mine);
+}
+
+// ---------------------------------------------------------------------------
+// cast_kv_append, e4m3 cache
+// ---------------------------------------------------------------------------
+// v as an e4m3 code (nearest even) under 1/scale `inv`; two per call.  The unit saturates
+// nothing here: |v * inv| <= 448 for finite v.
+__device__ __forceinline__ uint32_t code1(float v, float inv) {
+  const uint32_t c = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v * inv, 0.0f, 0, false) & 0xffu;
+  return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? 0x7fu : c;
+}
+__device__ __forceinline__ float exp_scale(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// the least e >= -117 with top <= 448 * 2^e (448 = 0.875 * 2^9)
+__device__ __forceinline__ int need_exp(float top) {
+  if (!(top > 0.0f)) return -117;
+  int e;
+  const float m = frexpf(top, &e);
+  return max(e - 9 + (m > 0.875f ? 1 : 0), -117);
+}
+
+// Eight channels [8c, 8c + 8) of one head's row, rotated (or not) in registers; the angles
+// are formed on the spot, v_sin and v_cos taking revolutions (their error, 2^-20 or so, is far
+// below the 2^-4 of the codes).
+__device__ __forceinline__ void rotated8(const uint16_t* x, int c, const Rope& r, long long pos_row,
+                                         int index, float* y) {
+  load8(x + 8 * c, y);
+  if (8 * c >= r.rot) return;
+  auto turn = [&](int j) -> f32x2 {
+    const int p = r.pos != nullptr ? r.pos[pos_row * r.n_axes + rope_axis(r, j)] : index;
+    const float f = rope_revs(r.turns[j], p);
+    return f32x2{__builtin_amdgcn_cosf(f) * r.amp, __builtin_amdgcn_sinf(f) * r.amp};
+  };
+  if (r.inter) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (8 * c + 2 * e < r.rot) {
+        const f32x2 t = turn(4 * c + e);
+        const float u = y[2 * e], w = y[2 * e + 1];
+        y[2 * e] = fmaf(u, t.x, -(w * t.y));
+        y[2 * e + 1] = fmaf(u, t.y, w * t.x);
+      }
+    }
+    return;
+  }
+  const int half = r.rot >> 1;
+  float o[8];
+  if (half % 8 == 0) {
+    load8(x + (8 * c < half ? 8 * c + half : 8 * c - half), o);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int ch = 8 * c + e;
+      o[e] = ch < r.rot ? to_f32(x[ch < half ? ch + half : ch - half]) : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int ch = 8 * c + e;
+    if (ch < half) {
+      const f32x2 t = turn(ch);
+      y[e] = fmaf(y[e], t.x, -(o[e] * t.y));
+    } else if (ch < r.rot) {
+      const f32x2 t = turn(ch - half);
+      y[e] = fmaf(o[e], t.y, y[e] * t.x);
+    }
+  }
+}
+
+// One block per (page of a sequence that the call writes, head, K or V): the largest
+// magnitude of the page's new tokens gives the exponent, then the codes are written.  The
+// call's pages of sequence b are numbered from cu[b] / page + 2 b (a sequence of n tokens
+// meets at most ceil(n / page) + 1 pages, so the ranges do not meet).  Up to kKeep chunks
+// of eight channels a thread stay in registers between the two passes; longer pages are
+// read again (from the L2).
+constexpr int kKeep = 4;
+__global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a) {
+  __shared__ f32x2 cs[kTok][kMaxPairs];
+  __shared__ int index[kTok], slot[kTok], mine[kTok];
+  __shared__ float tops[kThreads / 64];
+  const int nq = a.q_blocks_x * a.q_shares;
+  if ((int)blockIdx.x < nq) {
+    append_rows(a, blockIdx.x % a.q_blocks_x, blockIdx.x / a.q_blocks_x, 2 * a.H, cs, index, slot, mine);
+    return;
+  }
+  const int unit = blockIdx.x - nq;
+  const int x = unit / (2 * a.H), rem = unit - x * 2 * a.H;
+  const bool is_v = rem >= a.H;
+  const int h = is_v ? rem - a.H : rem;
+  const int b = find_seq(a.s.n_seq, x, [&](int i) { return div_by(seq_row(a.s, i), a.s.page) + 2 * i; });
+  const int beg = seq_row(a.s, b), end = seq_row(a.s, b + 1), len = seq_len(a.s, b);
+  const int first = max(len - (end - beg), 0);   // rows before token 0 are dropped
+  const int p = div_by(first, a.s.page) + (x - (div_by(beg, a.s.page) + 2 * b));
+  const int lo = max(first, p * a.page), hi = min(len, (p + 1) * a.page);
+  if (x < div_by(beg, a.s.page) + 2 * b || end <= beg || lo >= hi) return;
+  const int id = a.s.table[(long long)b * a.s.max_pages + p];
+  if (id < 0 || id >= a.pages) return;
+  const int had = lo - p * a.page;
+  const int row0 = end - (len - lo);             // the call's row of token lo
+  const int cpr = a.dh >> 3, total = (hi - lo) * cpr;
+  const uint16_t* src = is_v ? a.v + h * a.dh : a.k + h * a.dh;
+  const long long ss = is_v ? a.vs : a.ks;
+  uint8_t* page = static_cast<uint8_t*>(is_v ? a.vc : a.kc) + ((long long)id * a.page * a.H + h) * a.dh;
+  uint8_t* ep = (is_v ? a.ve : a.ke) + (long long)id * a.H + h;
+  const long long cs_row = (long long)a.H * a.dh;
+  const int shift = 31 - __clz(cpr);
+  auto get = [&](int i, float* y) {
+    const int t = i >> shift, c = i & (cpr - 1);
+    const uint16_t* xr = src + (long long)(row0 + t) * ss;
+    if (is_v || a.r.rot == 0) load8(xr + 8 * c, y);
+    else rotated8(xr, c, a.r, row0 + t, lo + t, y);
+  };
+  float keep[kKeep][8];
+  float top = 0.0f;
+  auto look = [&](const float* y) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float m = fabsf(y[e]);
+      top = m < INFINITY ? fmaxf(top, m) : top;   // false for NaN, too
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < kKeep; ++j) {
+    const int i = threadIdx.x + j * kThreads;
+    if (i < total) {
+      get(i, keep[j]);
+      look(keep[j]);
+    }
+  }
+  for (int i = threadIdx.x + kKeep * kThreads; i < total; i += kThreads) {
+    float y[8];
+    get(i, y);
+    look(y);
+  }
+  const int old = min((int)*ep, 247) - 127;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();                               // (also: every thread has read the old exponent)
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) top = fmaxf(top, tops[w]);
+  const int need = need_exp(top), e = had > 0 ? max(old, need) : need;
+  if (threadIdx.x == 0) *ep = (uint8_t)(e + 127);
+  const float inv = exp_scale(-e);
+  auto put = [&](int i, const float* y) {
+    const int t = i >> shift, c = i & (cpr - 1);
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k >> 2] |= code1(y[k], inv) << (8 * (k & 3));
+    *reinterpret_cast<u32x2*>(page + (had + t) * cs_row + 8 * c) = u32x2{w[0], w[1]};
+  };
+#pragma unroll
+  for (int j = 0; j < kKeep; ++j) {
+    const int i = threadIdx.x + j * kThreads;
+    if (i < total) put(i, keep[j]);
+  }
+  for (int i = threadIdx.x + kKeep * kThreads; i < total; i += kThreads) {
+    float y[8];
+    get(i, y);
+    put(i, y);
+  }
+  // earlier tokens of the page, rounded to the larger exponent
+  if (had > 0 && e > old) {
+    const float down = e - old < 127 ? exp_scale(old - e) : 0.0f;
+    for (int i = threadIdx.x; i < had * cpr; i += kThreads) {
+      u32x2* at = reinterpret_cast<u32x2*>(page + (i >> shift) * cs_row + 8 * (i & (cpr - 1)));
+      const u32x2 w = *at;
+      u32x2 o{0u, 0u};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const f32x2 f = k % 2 == 0 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k >> 1], false)
+                                   : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k >> 1], true);
+        o[k >> 1] |= (code1(f.x, down) | code1(f.y, down) << 8) << (16 * (k & 1));
+      }
+      *at = o;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// cast_kv_read
+// ---------------------------------------------------------------------------
+// A thread writes 16-byte chunks (eight channels), a block's width apart, so a wave writes
+// 1 KB in a row; grid (parts of a page, page, K or V).
+struct ReadArgs {
+  const void* k;
+  const void* v;
+  const uint8_t* ke;
+  const uint8_t* ve;
+  const int32_t* idx;
+  uint16_t* ko;
+  uint16_t* vo;
+  int pages, H;
+  long long chunks;              // 16-byte chunks of bf16 in a page
+  int cph_log2;                  // chunks per head
+  FastDiv heads;                 // by H
+};
+
+template <bool F8>
+__global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
+  const bool is_v = a.ko == nullptr || blockIdx.z == 1;
+  const int i = blockIdx.y;
+  const int id = a.idx[i];
+  uint16_t* out = (is_v ? a.vo : a.ko) + (long long)i * a.chunks * 8;
+  const long long step = (long long)gridDim.x * kThreads;
+  if (id < 0 || id >= a.pages) {
+    for (long long c = (long long)blockIdx.x * kThreads + threadIdx.x; c < a.chunks; c += step)
+      *reinterpret_cast<u32x4*>(out + 8 * c) = u32x4{0u, 0u, 0u, 0u};
+    return;
+  }
+  const uint8_t* src = static_cast<const uint8_t*>(is_v ? a.v : a.k) + (long long)id * a.chunks * (F8 ? 8 : 16);
+  const uint8_t* ex = F8 ? (is_v ? a.ve : a.ke) + (long long)id * a.H : nullptr;
+#pragma unroll 4
+  for (long long c = (long long)blockIdx.x * kThreads + threadIdx.x; c < a.chunks; c += step) {
+    if constexpr (F8) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(src + 8 * c);
+      const int at = (int)(c >> a.cph_log2), head = at - div_by(at, a.heads) * a.H;   // at: token and head
+      const float sc = __uint_as_float((uint32_t)ex[head] << 23);
+      u32x4 o;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const f32x2 f = k % 2 == 0 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k >> 1], false)
+                                   : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k >> 1], true);
+        o[k] = pack_bf16(f.x * sc, f.y * sc);
+      }
+      *reinterpret_cast<u32x4*>(out + 8 * c) = o;
+    } else {
+      *reinterpret_cast<u32x4*>(out + 8 * c) = *reinterpret_cast<const u32x4*>(src + 16 * c);
+    }
+  }
+}
+
+Rope make_rope(const cast_rope_params_t* p, const int32_t* pos, int transpose) {
+  Rope r{};
+  if (p == nullptr) return r;
+  r.turns = p->turns;
+  r.axis = p->n_axes > 1 ? p->axis : nullptr;
+  r.pos = pos;
+  r.rot = p->rot_dim;
+  r.inter = p->interleaved;
+  r.n_axes = p->n_axes;
+  r.amp = p->amplitude;
+  r.sign = transpose ? -1.0f : 1.0f;
+  return r;
+}
+
+// heads per block: all of them once there are blocks for every compute unit several
+// times over, else shared out down to about two items a thread
+int heads_per_block(int tok_blocks, int heads, int per_head) {
+  const int least = std::max(1, 2 * kThreads / (kTok * per_head));
+  int shares = std::max(1, 1024 / std::max(tok_blocks, 1));
+  int hpb = (heads + shares - 1) / shares;
+  return std::min(std::max(hpb, least), heads);
+}
+
+}  // namespace
+
+KvSeqs make_seqs(const cast_kv_seqs_t& s, int page) {
+  return KvSeqs{s.cu, s.len, s.table, s.n_seq, s.n_tok, s.max_pages, s.max_pages * page, fast_div(page)};
+}
+
+cast_status_t launch_rope(const void* x, int dtype, int n, int H, int dh, long long xt, long long xh,
+                          const int32_t* pos, const cast_rope_params_t& p, int transpose, void* out,
+                          long long yt, long long yh, bool wide, hipStream_t stream) {
+  const Rope r = make_rope(&p, pos, transpose);
+  const Items it = plan_items(r.rot, r.inter, dh, wide);
+  const int bx = (n + kTok - 1) / kTok, heads = heads_per_block(bx, H, it.per_head);
+  const dim3 grid(bx, (H + heads - 1) / heads);
+  if (dtype == 0)
+    hipLaunchKernelGGL((rope_kernel<float>), grid, dim3(kThreads), 0, stream, static_cast<const float*>(x), xt, xh,
+                       static_cast<float*>(out), yt, yh, n, H, heads, r, it);
+  else
+    hipLaunchKernelGGL((rope_kernel<uint16_t>), grid, dim3(kThreads), 0, stream, static_cast<const uint16_t*>(x), xt,
+                       xh, static_cast<uint16_t*>(out), yt, yh, n, H, heads, r, it);
+  return check_launch("rope");
+}
+
+cast_status_t launch_kv_append(const cast_kv_cache_t& c, const cast_kv_seqs_t& s, const void* k, long long ks,
+                               const void* v, long long vs, const cast_rope_params_t* rope, const int32_t* pos,
+                               const void* q, long long qs, int Hq, void* q_out, hipStream_t stream) {
+  AppendArgs a{};
+  a.s = make_seqs(s, c.page);
+  a.r = make_rope(rope, pos, 0);
+  a.it = plan_items(a.r.rot, a.r.inter, c.dh, true);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.kc = c.k;
+  a.vc = c.v;
+  a.ke = c.k_exp;
+  a.ve = c.v_exp;
+  a.ks = ks;
+  a.vs = vs;
+  a.qs = qs;
+  a.H = c.H;
+  a.Hq = q != nullptr ? Hq : 0;
+  a.dh = c.dh;
+  a.pages = c.pages;
+  a.page = c.page;
+  const int bx = (s.n_tok + kTok - 1) / kTok;
+  if (c.dtype == 1) {
+    const int all = 2 * c.H + a.Hq;
+    a.heads = heads_per_block(bx, all, a.it.per_head);
+    hipLaunchKernelGGL(append_kernel, dim3(bx, (all + a.heads - 1) / a.heads), dim3(kThreads), 0, stream, a);
+  } else {
+    if (a.Hq > 0) {
+      a.heads = heads_per_block(bx, a.Hq, a.it.per_head);
+      a.q_blocks_x = bx;
+      a.q_shares = (a.Hq + a.heads - 1) / a.heads;
+    }
+    // every group of the call holds a token, or is a sequence's first or last page
+    const long long groups = (long long)s.n_tok / c.page + 2ll * s.n_seq;
+    const long long blocks = (long long)a.q_blocks_x * a.q_shares + groups * 2 * c.H;
+    if (blocks >= (1ll << 31)) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
+    hipLaunchKernelGGL(append8_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  }
+  return check_launch("kv_append");
+}
+
+cast_status_t launch_kv_read(const cast_kv_cache_t& c, const int32_t* idx, int m, void* ko, void* vo,
+                             hipStream_t stream) {
+  ReadArgs a{};
+  a.k = c.k;
+  a.v = c.v;
+  a.ke = c.k_exp;
+  a.ve = c.v_exp;
+  a.idx = idx;
+  a.ko = static_cast<uint16_t*>(ko);
+  a.vo = static_cast<uint16_t*>(vo);
+  a.pages = c.pages;
+  a.H = c.H;
+  a.cph_log2 = c.dh == 32 ? 2 : c.dh == 64 ? 3 : 4;
+  a.heads = fast_div(c.H);
+  a.chunks = (long long)c.page * c.H << a.cph_log2;
+  const unsigned parts = (unsigned)std::min<long long>((a.chunks + 4 * kThreads - 1) / (4 * kThreads), 65535);
+  const unsigned z = ko != nullptr && vo != nullptr ? 2 : 1;
+  // pages beyond the grid's limit of rows go in further launches
+  for (int at = 0; at < m; at += 65535) {
+    ReadArgs b = a;
+    b.idx = idx + at;
+    if (ko != nullptr) b.ko = a.ko + (long long)at * a.chunks * 8;
+    if (vo != nullptr) b.vo = a.vo + (long long)at * a.chunks * 8;
+    const dim3 grid(parts, (unsigned)std::min(m - at, 65535), z);
+    if (c.dtype == 2) hipLaunchKernelGGL((read_kernel<true>), grid, dim3(kThreads), 0, stream, b);
+    else hipLaunchKernelGGL((read_kernel<false>), grid, dim3(kThreads), 0, stream, b);
+  }
+  return check_launch("kv_read");
+}
+
+}  // namespace cast

@@ -1,0 +1,77 @@
+// Device code shared by the cached-history kernels: sequence lookup, page lookup and the
+// rotation's angles.
+#pragma once
+
+#include "cast_common.h"
+
+namespace cast {
+
+// Division of 0 <= x by a fixed d >= 1 through one 64-bit product: exact for x * d < 2^40
+// and x < 2^24 d (the entry points refuse sizes past that).
+struct FastDiv {
+  unsigned long long magic;
+  int d;
+};
+inline FastDiv fast_div(int d) {
+  return FastDiv{((1ull << 40) + (unsigned long long)d - 1) / (unsigned long long)d, d};
+}
+__device__ __forceinline__ int div_by(int x, FastDiv f) {
+  return (int)(((unsigned long long)(unsigned)x * f.magic) >> 40);
+}
+
+// The sequences of a call as the kernels read them.  Garbage in the device arrays gives
+// garbage results, never an access outside the tensors.
+struct KvSeqs {
+  const int32_t* cu;
+  const int32_t* len;
+  const int32_t* table;
+  int n_seq, n_tok, max_pages;
+  int max_tokens;                // max_pages * page
+  FastDiv page;
+};
+
+__device__ __forceinline__ int seq_row(const KvSeqs& s, int b) { return min(max(s.cu[b], 0), s.n_tok); }
+__device__ __forceinline__ int seq_len(const KvSeqs& s, int b) { return min(max(s.len[b], 0), s.max_tokens); }
+
+// The last b in [0, n_seq) with start(b) <= x, for a start() that does not decrease and
+// start(0) <= x: 64 probes per step, one per lane (one step up to 64 sequences).  Every
+// lane of the wave calls it with the same x.
+template <class F>
+__device__ __forceinline__ int find_seq(int n_seq, int x, F&& start) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, cnt = n_seq;
+  while (cnt > 1) {
+    const int step = (cnt + 63) >> 6;
+    const int b = lo + lane * step;
+    const unsigned long long hit = __ballot(b < lo + cnt && start(b) <= x);
+    const int c = max(__popcll(hit), 1);
+    const int at = (c - 1) * step;
+    lo += at;
+    cnt = min(step, cnt - at);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// The rotation as the kernels read it.
+struct Rope {
+  const double* turns;
+  const uint8_t* axis;
+  const int32_t* pos;            // [n, n_axes], or NULL: the token's index in its sequence
+  int rot, inter, n_axes;
+  float amp;
+  float sign;                    // -1: transposed
+};
+
+__device__ __forceinline__ int rope_axis(const Rope& r, int j) {
+  return r.axis == nullptr ? 0 : min((int)r.axis[j], r.n_axes - 1);
+}
+
+// The angle of pair j at position p, in revolutions of [-0.5, 0.5]: the product and its
+// reduction are fp64 (fp32 would keep no angle at all of p = 10^6 and turns ~ 0.16: its
+// product is off by 2^-24 * 1.6e5 = 0.01 revolutions).
+__device__ __forceinline__ float rope_revs(double turns, int p) {
+  const double t = (double)p * turns;
+  return (float)(t - rint(t));
+}
+
+}  // namespace cast
