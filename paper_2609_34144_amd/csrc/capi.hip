@@ -724,6 +724,8 @@ static cast_status_t kv_attn_sizes(const cast_kv_cache_t* cache, const cast_kv_s
     return fail(CAST_ERR_SHAPE, "kv_attn: Hq must be a multiple of the cache's %d heads, at most 65536 (got %d)", cache->H, Hq);
   if ((long long)seqs->n_tok * Hq >= (1LL << 31))
     return fail(CAST_ERR_UNSUPPORTED, "kv_attn: n_tok * Hq must stay below 2^31");
+  if (((long long)seqs->n_tok * (Hq / cache->H) / 16 + seqs->n_seq) * cache->H >= (1LL << 30))
+    return fail(CAST_ERR_UNSUPPORTED, "kv_attn: too many row tiles");
   if (max_len < 1) return fail(CAST_ERR_SHAPE, "kv_attn: max_len must be >= 1 (got %d)", max_len);
   if (causal != 0 && causal != 1) return fail(CAST_ERR_SHAPE, "kv_attn: causal must be 0 or 1");
   if (window < 0 || sinks < 0) return fail(CAST_ERR_SHAPE, "kv_attn: window and sinks must be >= 0");
@@ -761,10 +763,11 @@ cast_status_t cast_kv_attn(const void* q, long long q_stride, int Hq, const cast
   KvAttnPlan plan = make_kv_attn_plan(cache, seqs, Hq, max_len, window, sinks);
   if (workspace == nullptr) {
     plan.pieces = 1;                               // every row tile whole
+    plan.target = 0;
   } else {
     if (!aligned(workspace, kWsAlign))
       return fail(CAST_ERR_WORKSPACE, "kv_attn: workspace must be %zu-byte aligned", kWsAlign);
-    if (plan.pieces > 1 && workspace_bytes < plan.bytes)
+    if (plan.cut() && workspace_bytes < plan.bytes)
       return fail(CAST_ERR_WORKSPACE, "kv_attn: workspace has %zu bytes, %zu needed", workspace_bytes, plan.bytes);
   }
   return launch_kv_attn(q, q_stride, Hq, *cache, *seqs, causal, std::min(window, 1 << 30), sinks, scale, out, lse_out,

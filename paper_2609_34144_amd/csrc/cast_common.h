@@ -166,10 +166,12 @@ KvSeqs make_seqs(const cast_kv_seqs_t& s, int page);
 // How a call of cast_kv_attn is cut up.  `bytes` of workspace hold this plan and that of any
 // smaller max_len.
 struct KvAttnPlan {
-  bool few_rows;                 // 32-row workgroups (else 128)
-  int row_tiles;                 // upper bound over all ways to share the rows out
-  int pieces, piece_tiles;       // pieces along the keys, key tiles of each
-  size_t part_bytes, bytes;
+  int rows;                      // rows per workgroup: 16 or 32 (few rows), 128
+  int row_tiles;                 // at most, over all ways to share the rows out
+  int pieces, piece_tiles;       // 128 rows: pieces along the keys, key tiles of each
+  int target, max_items;         // few rows: pieces wanted (0: none is cut), work items at most
+  size_t part_bytes, lse_bytes, bytes;
+  bool cut() const { return pieces > 1 || target > 0; }
 };
 KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, long long max_len, int window,
                         int sinks, int cus);

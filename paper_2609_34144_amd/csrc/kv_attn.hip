@@ -15,9 +15,9 @@
 // Two kernels:
 //   tiles  128 rows per workgroup; its four waves share 64-key tiles in LDS, copied one
 //          tile ahead.  Bound by the matrix cores and the softmax's VALU work.
-//   rows   32 rows per workgroup (few rows: decoding); each wave takes every fourth 32-key
-//          tile by itself, keys straight from memory into MFMA operands, values through a
-//          private LDS tile; no barrier until the four results are joined.  Bound by HBM.
+//   rows   16 or 32 rows per workgroup (few rows: decoding); each wave takes every fourth
+//          32-key tile by itself, keys straight from memory into MFMA operands, values through
+//          a private LDS tile; no barrier until the four results are joined.  Bound by HBM.
 // Long key ranges with few row tiles are cut into pieces, joined by a second kernel.
 #include <algorithm>
 #include <utility>
@@ -44,8 +44,7 @@ typedef __attribute__((address_space(3))) char lds_char;
 constexpr int kThreads = 256;
 constexpr int kTileRows = 128;   // rows per workgroup of the tiles kernel
 constexpr int kTileKeys = 64;
-constexpr int kRows = 32;        // of the rows kernel
-constexpr int kRowKeys = 32;     // keys per tile and wave there
+constexpr int kRowKeys = 32;     // keys per tile and wave of the rows kernel
 constexpr int kMaxPieces = 128;
 // s_waitcnt vmcnt(0) that leaves expcnt and lgkmcnt free
 constexpr int kVmcnt0 = 0x0F70;
@@ -65,11 +64,13 @@ struct KvAttnArgs {
   KvSeqs s;
   uint16_t* out;
   float* lse;
-  float* part_o;                 // [pieces][n_tok * Hq][dh], normalised
-  float* part_lse;               // [pieces][n_tok * Hq], log2 domain
+  float* part_o;                 // normalised: [pieces][n_tok * Hq][dh], or [items][rows][dh]
+  float* part_lse;               // log2 domain: [pieces][n_tok * Hq], or [items][rows]
   int Hq, H, g, pages, page;
   int causal, window, sinks;     // window 0: none
-  int npieces, piece_tiles;
+  int npieces, piece_tiles;      // tiles kernel: pieces along the keys, key tiles of each
+  int target, max_items;         // rows kernel: pieces wanted (0: none is cut), items at most
+  int2* meta;                    // rows kernel: first item and pieces of [row tile][KV head]
   float sl2;                     // scale * log2(e)
 };
 
@@ -116,28 +117,42 @@ struct RowTile {
   int len, off;                  // its length; position of its first token of the call
   int ts, tw, nt;                // logical key tile u: u < ts ? u : tw + u - ts; nt in all
 };
-// x-th row tile of the call (tiles of TM rows; sequence b's are numbered from
-// floor(cu[b] g / TM) + b, which leaves room for its partial tile)
-template <int TM, int TK>
-__device__ __forceinline__ bool row_tile(const KvAttnArgs& a, int x, RowTile& t) {
-  auto start = [&](int i) { return (int)((unsigned)(seq_row(a.s, i) * a.g) / (unsigned)TM) + i; };
-  t.b = find_seq(a.s.n_seq, x, start);
-  t.beg = seq_row(a.s, t.b);
-  const int n = max(seq_row(a.s, t.b + 1) - t.beg, 0), k = x - start(t.b);
-  t.n_rows = n * a.g;
-  if (k < 0 || (long long)k * TM >= t.n_rows) return false;
-  t.row0 = k * TM;
-  t.len = seq_len(a.s, t.b);
-  t.off = t.len - n;
-  const int p_lo = t.off + t.row0 / a.g, p_hi = t.off + (min(t.row0 + TM, t.n_rows) - 1) / a.g;
-  const int hi = max(a.causal ? min(p_hi + 1, t.len) : t.len, 0);
+// the key tiles that rows at positions p_lo .. p_hi of a sequence of `len` meet
+template <int TK>
+__device__ __forceinline__ void key_tiles(const KvAttnArgs& a, RowTile& t, int p_lo, int p_hi, int len) {
+  const int hi = max(a.causal ? min(p_hi + 1, len) : len, 0);
   const int lo = a.window > 0 ? min(max(p_lo - a.window + 1, 0), hi) : 0;
   const int sk = a.window > 0 ? min(a.sinks, hi) : 0;
   const int te = (hi + TK - 1) / TK;
   t.ts = (sk + TK - 1) / TK;
   t.tw = max(lo / TK, t.ts);
   t.nt = t.ts + max(te - t.tw, 0);
+}
+// Row tiles of the call: those of sequence b are numbered from floor(cu[b] g / TM) + b,
+// which leaves room for its partial tile.
+template <int TM>
+__device__ __forceinline__ int first_tile(const KvAttnArgs& a, int b) {
+  return (int)((unsigned)(seq_row(a.s, b) * a.g) / (unsigned)TM) + b;
+}
+// row tile k of sequence b
+template <int TM, int TK>
+__device__ __forceinline__ bool place(const KvAttnArgs& a, int b, int k, RowTile& t) {
+  t.b = b;
+  t.beg = seq_row(a.s, b);
+  const int n = max(seq_row(a.s, b + 1) - t.beg, 0);
+  t.n_rows = n * a.g;
+  if (k < 0 || (long long)k * TM >= t.n_rows) return false;
+  t.row0 = k * TM;
+  t.len = seq_len(a.s, b);
+  t.off = t.len - n;
+  key_tiles<TK>(a, t, t.off + t.row0 / a.g, t.off + (min(t.row0 + TM, t.n_rows) - 1) / a.g, t.len);
   return true;
+}
+// x-th row tile of the call
+template <int TM, int TK>
+__device__ __forceinline__ bool row_tile(const KvAttnArgs& a, int x, RowTile& t) {
+  const int b = find_seq(a.s.n_seq, x, [&](int i) { return first_tile<TM>(a, i); });
+  return place<TM, TK>(a, b, x - first_tile<TM>(a, b), t);
 }
 // logical key tiles [u0, u1) of piece z
 __device__ __forceinline__ void piece_range(const KvAttnArgs& a, int nt, int z, int& u0, int& u1) {
@@ -168,20 +183,24 @@ __device__ __forceinline__ int tile_kind(const KvAttnArgs& a, int j0, int p0, in
   return full ? 2 : 1;
 }
 
+// The lane's visible keys among j0 .. j0 + 31 as bits (of those in `there`).
+__device__ __forceinline__ uint32_t below(int n) {   // bits 0 .. n - 1
+  return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u;
+}
+__device__ __forceinline__ uint32_t visible_bits(RowLimits r, int sinks, int j0, uint32_t there) {
+  return there & below(r.hi - j0) & (~below(r.lo - j0) | below(sinks - j0));
+}
 // S^T accumulator element e of block kb belongs to key kb * 32 + 8 (e / 4) + 4 hf + e % 4.
 template <int NB>
 __device__ __forceinline__ void mask_scores(f32x16 (&sn)[NB], int j0, int hf, RowLimits r, int sinks,
                                             unsigned long long there) {
-  const unsigned long long bits = there >> (4 * hf);
 #pragma unroll
-  for (int kb = 0; kb < NB; ++kb)
+  for (int kb = 0; kb < NB; ++kb) {
+    const uint32_t bits = visible_bits(r, sinks, j0 + 32 * kb, (uint32_t)(there >> (32 * kb))) >> (4 * hf);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int c = kb * 32 + 8 * (e / 4) + e % 4;
-      const int key = j0 + c + 4 * hf;
-      const bool seen = key < r.hi && (key >= r.lo || key < sinks) && ((bits >> c) & 1) != 0;
-      if (!seen) sn[kb][e] = -INFINITY;
-    }
+    for (int e = 0; e < 16; ++e)
+      if (((bits >> (8 * (e / 4) + e % 4)) & 1) == 0) sn[kb][e] = -INFINITY;
+  }
 }
 
 // Exponentials of a tile against the running maximum, packed as P^T operands, and their
@@ -248,54 +267,74 @@ __device__ __forceinline__ void values(R&& read, const bf16x8 (&pp)[NB][2], f32x
   });
 }
 
-// The same where some row does not see some key.  There P = 0, and 0 times an infinity or
-// NaN that lies at the invisible place must add nothing: the tile's product is formed
-// apart, and if it is not finite, from the finite values plus the signs of the others at
-// the keys whose weight is not zero (both signs, or a NaN, give NaN).
+// Infinities and NaN at places that a row does not see must add nothing to it, but there
+// P = 0 and 0 * inf is NaN.  So a tile that some row sees only in part is looked through for
+// them (exponent bits all set), and if it holds any its product is formed in three: the
+// finite values, and 0/1 images of where +inf (or NaN) and -inf (or NaN) lie under 0/1
+// weights; a row that meets only +inf gets that, only -inf that, both or a NaN a NaN.
+__device__ __forceinline__ uint32_t special_bits(uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; }   // bits 15, 31
+__device__ __forceinline__ uint32_t special_bits(bf16x8 op) {
+  const u32x4 w = __builtin_bit_cast(u32x4, op);
+  return (special_bits(w.x) | special_bits(w.y)) | (special_bits(w.z) | special_bits(w.w));
+}
+struct Images {
+  bf16x8 fin, pos, neg;
+};
+__device__ __forceinline__ Images images(bf16x8 op) {
+  const u32x4 w = __builtin_bit_cast(u32x4, op);
+  u32x4 f, p, n;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t m = special_bits(w[i]) & 0x80008000u;
+    const uint32_t nan = m & (((w[i] & 0x007f007fu) + 0x007f007fu) << 8), sign = w[i] & 0x80008000u;
+    f[i] = w[i] & ~((m >> 15) * 0xffffu);
+    p[i] = ((m & (~sign | nan)) >> 15) * 0x3f80u;
+    n[i] = ((m & (sign | nan)) >> 15) * 0x3f80u;
+  }
+  return Images{__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, p), __builtin_bit_cast(bf16x8, n)};
+}
+// 1 where a weight is not zero
+__device__ __forceinline__ bf16x8 seen_weights(bf16x8 p8) {
+  u32x4 p = __builtin_bit_cast(u32x4, p8);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = ((((p[i] & 0x7fff7fffu) + 0x7fff7fffu) & 0x80008000u) >> 15) * 0x3f80u;
+  return __builtin_bit_cast(bf16x8, p);
+}
+// pos, neg: counts; one above 0 times 3e38 twice is infinite (not fused with the sums, which
+// would take the product without its overflow)
+template <int N, class V>
+__device__ __forceinline__ void add_special(V& acc, V pos, V neg) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float p = pos[e] * 3.0e38f, n = neg[e] * 3.0e38f;
+    acc[e] += p * 3.0e38f - n * 3.0e38f;
+  }
+  asm volatile("" : "+v"(acc));   // done before the next block of channels begins: fewer registers
+}
 template <int NB, int ND, class R>
-__device__ __forceinline__ void values_masked(R&& read, const bf16x8 (&pp)[NB][2], f32x16 (&acc)[ND]) {
+__device__ __forceinline__ bool has_special(R&& read) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int g = 0; g < 2 * NB; ++g)
+#pragma unroll
+    for (int db = 0; db < ND; ++db) m |= special_bits(read(db, g / 2, g % 2));
+  return __ballot((m & 0x80008000u) != 0) != 0ull;
+}
+template <int NB, int ND, class R>
+__device__ __forceinline__ void values_special(R&& read, const bf16x8 (&pp)[NB][2], f32x16 (&acc)[ND]) {
 #pragma unroll
   for (int db = 0; db < ND; ++db) {
-    f32x16 t{};
+    f32x16 pos{}, neg{};
 #pragma unroll
-    for (int g = 0; g < 2 * NB; ++g) t = mfma(read(db, g / 2, g % 2), pp[g / 2][g % 2], t);
-    bool bad = false;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) bad |= !(fabsf(t[e]) < INFINITY);
-    if (__ballot(bad) != 0ull) {
-      f32x16 fin{}, pos{}, neg{};
-#pragma unroll 1
-      for (int g = 0; g < 2 * NB; ++g) {
-        u32x4 v = __builtin_bit_cast(u32x4, read(db, g / 2, g % 2)), vp, vn, w;
-        bf16x8 p8 = pp[0][0];
-#pragma unroll
-        for (int x = 1; x < 2 * NB; ++x)
-          if (g == x) p8 = pp[x / 2][x % 2];
-        const u32x4 p = __builtin_bit_cast(u32x4, p8);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          vp[i] = vn[i] = w[i] = 0;
-#pragma unroll
-          for (int s = 0; s < 32; s += 16) {
-            const uint32_t one = 0x3f80u << s, x = (v[i] >> s) & 0xffffu;
-            if ((x & 0x7f80u) == 0x7f80u) {
-              if (x != 0xff80u) vp[i] |= one;
-              if (x != 0x7f80u) vn[i] |= one;
-              v[i] &= ~(0xffffu << s);
-            }
-            if (((p[i] >> s) & 0x7fffu) != 0) w[i] |= one;
-          }
-        }
-        const bf16x8 seen = __builtin_bit_cast(bf16x8, w);
-        fin = mfma(__builtin_bit_cast(bf16x8, v), p8, fin);
-        pos = mfma(__builtin_bit_cast(bf16x8, vp), seen, pos);
-        neg = mfma(__builtin_bit_cast(bf16x8, vn), seen, neg);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        t[e] = (fin[e] + (pos[e] > 0.0f ? INFINITY : 0.0f)) + (neg[e] > 0.0f ? -INFINITY : 0.0f);
+    for (int g = 0; g < 2 * NB; ++g) {
+      const Images v = images(read(db, g / 2, g % 2));
+      const bf16x8 w = seen_weights(pp[g / 2][g % 2]);
+      acc[db] = mfma(v.fin, pp[g / 2][g % 2], acc[db]);
+      pos = mfma(v.pos, w, pos);
+      neg = mfma(v.neg, w, neg);
     }
-    acc[db] += t;
+    add_special<16>(acc[db], pos, neg);
   }
 }
 
@@ -414,12 +453,14 @@ __global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
     const int c = 2 * (gq & 1) + ((la & 3) >> 1);
     vbase = (unsigned)(vr * ROWB + ((c ^ vswz(vr, CPR)) * 16) + 8 * (la & 1));
   }
-  auto read_k = [&](const uint16_t* kt, int i, int kb) __attribute__((always_inline)) -> bf16x8 {
+  // (the XORs are formed again at each use: opaque() keeps them out of registers across the loop)
+  auto opaque = [](unsigned x) { asm volatile("" : "+v"(x)); return x; };
+  auto read_k = [&](const uint16_t* kt, unsigned kb0, int i, int kb) __attribute__((always_inline)) -> bf16x8 {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(
-        reinterpret_cast<const char*>(kt) + (kbase ^ (32u * i)) + kb * 32 * ROWB));
+        reinterpret_cast<const char*>(kt) + (kb0 ^ (32u * i)) + kb * 32 * ROWB));
   };
-  auto read_v = [&](const uint16_t* vt, int db, int kb, int s2) __attribute__((always_inline)) -> bf16x8 {
-    const lds_char* p = (const lds_char*)(vt) + (vbase ^ (64u * db)) + (32 * kb + 16 * s2) * ROWB;
+  auto read_v = [&](const uint16_t* vt, unsigned vb0, int db, int kb, int s2) __attribute__((always_inline)) -> bf16x8 {
+    const lds_char* p = (const lds_char*)(vt) + (vb0 ^ (64u * db)) + (32 * kb + 16 * s2) * ROWB;
     const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
     const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * ROWB)));
     return __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
@@ -466,19 +507,20 @@ __global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
     if (kind != 0) {
       f32x16 sn[2];
       constexpr int N = 2 * (DH / 16), AHEAD = 3;
+      const unsigned kb0 = opaque(kbase), vb0 = opaque(vbase);
       bf16x8 op[N];
-      static_for<0, AHEAD>([&](auto uu) { constexpr int i = decltype(uu)::value; op[i] = read_k(kt, i / 2, i % 2); });
+      static_for<0, AHEAD>([&](auto uu) { constexpr int i = decltype(uu)::value; op[i] = read_k(kt, kb0, i / 2, i % 2); });
       static_for<0, N>([&](auto uu) {
         constexpr int i = decltype(uu)::value, n = i + AHEAD;
-        if constexpr (n < N) op[n] = read_k(kt, n / 2, n % 2);
+        if constexpr (n < N) op[n] = read_k(kt, kb0, n / 2, n % 2);
         sn[i % 2] = mfma(op[i], qreg[i / 2], i < 2 ? f32x16{} : sn[i % 2]);
       });
       if (kind == 1) mask_scores<2>(sn, j0, hf, lim, a.sinks, there);
       bf16x8 pp[2][2];
       softmax<2, ND>(sn, pp, m_run, l_run, acc, a.sl2);
-      auto rd = [&](int db, int kb, int s2) __attribute__((always_inline)) { return read_v(vt, db, kb, s2); };
-      if (kind == 2) values<2, ND>(rd, pp, acc);
-      else values_masked<2, ND>(rd, pp, acc);
+      auto rd = [&](int db, int kb, int s2) __attribute__((always_inline)) { return read_v(vt, vb0, db, kb, s2); };
+      if (kind == 1 && has_special<2, ND>(rd)) values_special<2, ND>(rd, pp, acc);
+      else values<2, ND>(rd, pp, acc);
     }
     if constexpr (F8) {
       if (more) store8(kn, vn);
@@ -524,180 +566,362 @@ __global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
 // ---------------------------------------------------------------------------
 // rows
 // ---------------------------------------------------------------------------
-template <int DH, bool F8>
-__global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttnArgs a) {
-  constexpr int CPR = DH / 8, ROWB = DH * 2, ND = DH / 32, TK = kRowKeys, W = kThreads / 64;
-  constexpr int NK = F8 ? DH / 32 : DH / 16;         // 16-byte loads of a lane's key half
-  constexpr int CV = F8 ? DH / 16 : DH / 8;          // 16-byte chunks of a value row in memory
-  constexpr int NV = TK * CV / 64;                   // loads of a value tile per lane
-  constexpr int VSTEP = 64 / CV;                     // rows between them
-  // value tiles, one per wave; afterwards the waves' results
-  __shared__ __attribute__((aligned(1024))) char smem[W * kRows * DH * 4];
-  __shared__ float sm[W][kRows], sl[W][kRows];
+// v_mfma_f32_16x16x32_bf16: of 16 rows an accumulator takes a quarter of the registers that
+// 32x32 tiles need, which leaves room for three workgroups per compute unit, each wave with
+// a whole key tile on its way.  NQ blocks of 16 rows share every key read.
+//
+// Work list.  The call's work is shared out by the lengths the device sees, not by their
+// bound: with T the key tiles of all row tiles, a piece is P = max(kMinPiece, T H / target)
+// key tiles, so there are about `target` pieces of like size however ragged the batch.
+// (Cut by the bound on the lengths, 16 streams of 300 to 8100 tokens ran as 2048 workgroups
+// of at most 4 key tiles a wave, half of them empty: 154 us.)  Item x of the list:
+// sequence by sequence, row tile, piece, head (fastest, so that neighbours read
+// neighbouring rows of memory).
+constexpr int kMinPiece = 16;    // key tiles (of 32): four for each wave
 
+struct Item {
   RowTile t;
-  if (!row_tile<kRows, TK>(a, blockIdx.x, t)) return;
-  const int h = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  int h, z, pieces, item0;       // head, piece of `pieces`, item of piece 0 (the next: + H)
+  int tile_id, per;              // number of the row tile in the call, key tiles of a piece
+};
+struct SeqWork {
+  int rt, nt;
+};
+template <int TM>
+__device__ __forceinline__ SeqWork seq_work(const KvAttnArgs& a, int b) {
+  SeqWork w{0, 0};
+  if (b >= a.s.n_seq) return w;
+  const int beg = seq_row(a.s, b), n = seq_row(a.s, b + 1) - beg, len = seq_len(a.s, b);
+  if (n <= 0) return w;
+  w.rt = (n * a.g + TM - 1) / TM;
+  RowTile t;
+  key_tiles<kRowKeys>(a, t, len - n, len - 1, len);
+  w.nt = t.nt;
+  return w;
+}
+template <int TM>
+__device__ __forceinline__ bool find_item(const KvAttnArgs& a, int x, Item& it) {
+  const int lane = threadIdx.x & 63, n_seq = a.s.n_seq;
+  SeqWork w = seq_work<TM>(a, lane);
+  int per = 0x3fffffff;
+  if (a.target > 0) {
+    float sum = 0.0f;
+    for (int c = 0; c < n_seq; c += 64) {
+      const SeqWork v = c == 0 ? w : seq_work<TM>(a, c + lane);
+      sum += (float)v.rt * (float)v.nt;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    // (rounded up, so that the items never pass target + row tiles * H)
+    per = max(kMinPiece, (int)fminf(ceilf(sum * (float)a.H * 1.0001f / (float)a.target), 1.0e9f));
+  }
+  int base = 0;
+  for (int c = 0; c < n_seq; c += 64) {
+    if (c > 0) w = seq_work<TM>(a, c + lane);
+    const int pieces = max(1, (w.nt + per - 1) / per);
+    int incl = w.rt * pieces * a.H;
+    const int mine = incl;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    const unsigned long long hit = __ballot(x - base < incl);
+    if (hit != 0) {
+      const int l = __ffsll((long long)hit) - 1;
+      const int first = base + __shfl(incl - mine, l);
+      it.pieces = __builtin_amdgcn_readfirstlane(__shfl(pieces, l));
+      it.per = per;
+      const int local = __builtin_amdgcn_readfirstlane(x - first), rest = local / a.H;
+      it.h = local - rest * a.H;
+      const int k = rest / it.pieces;
+      it.z = rest - k * it.pieces;
+      it.item0 = __builtin_amdgcn_readfirstlane(first) + k * it.pieces * a.H + it.h;
+      it.tile_id = first_tile<TM>(a, c + l) + k;
+      return place<TM, kRowKeys>(a, c + l, k, it.t);
+    }
+    base += __shfl(incl, 63);
+  }
+  return false;
+}
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// max over the four quarters of a wave
+__device__ __forceinline__ float quarter_max(float x) {
+  const u32x2 s = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return half_swap_max(fmaxf(__uint_as_float(s.x), __uint_as_float(s.y)));
+}
+
+template <int DH, bool F8, int NQ>
+__global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAttnArgs a) {
+  constexpr int CPR = DH / 8, ROWB = DH * 2, TK = kRowKeys, W = kThreads / 64, TM = 16 * NQ;
+  constexpr int NT = DH / 32;                        // contraction steps of S, 32 channels each
+  constexpr int ND = DH / 16;                        // 16-channel blocks of O^T
+  // Loads of a lane: rows l16 and l16 + 16 of the tile; bf16 16 bytes (channels 32 i + 8
+  // quarter ..) for each step; codes 16 bytes (channels 64 i + 16 quarter ..) for two steps,
+  // or, of 32-wide heads, 8 bytes for the one step
+  constexpr int NL = F8 ? (DH == 32 ? 1 : DH / 64) : NT;
+  constexpr bool HALF = F8 && DH == 32;
+  __shared__ __attribute__((aligned(1024))) char smem[W * (TM * DH * 4 > TK * ROWB ? TM * DH * 4 : TK * ROWB)];
+  __shared__ float sm[W][TM], sl[W][TM];
+
+  Item it;
+  if (!find_item<TM>(a, blockIdx.x, it)) return;
+  const RowTile& t = it.t;
+  const int h = it.h, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, hf = lane >> 5;
-  int u0, u1;
-  piece_range(a, t.nt, blockIdx.z, u0, u1);
-  const int nrows = min(kRows, t.n_rows - t.row0);
-  const int r = t.row0 + min(l32, nrows - 1);
-  const int tok = r / a.g, hq = h * a.g + (r - tok * a.g);
+  const int l16 = lane & 15, qd = lane >> 4;
+  const int u0 = min(it.z * it.per, t.nt), u1 = min(u0 + min(it.per, t.nt), t.nt);
+  const int nrows = min(TM, t.n_rows - t.row0);
   const int p0 = t.off + t.row0 / a.g, p1 = t.off + (t.row0 + nrows - 1) / a.g;
-  const RowLimits lim = row_limits(a, t, t.off + tok);
-  // Q^T in the order in which the lane gets its key's channels: bf16 16 i + 8 hf ..; codes
-  // come 16 to a load, so 32 (i / 2) + 16 hf + 8 (i % 2) ..
-  bf16x8 qreg[DH / 16];
-  {
+  RowLimits lim[NQ];
+  bf16x8 qreg[NQ][NT];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    const int r = t.row0 + min(16 * nq + l16, nrows - 1);
+    const int tok = r / a.g, hq = h * a.g + (r - tok * a.g);
+    lim[nq] = row_limits(a, t, t.off + tok);
     const uint16_t* qp = a.q + (long long)(t.beg + tok) * a.qs + hq * DH;
 #pragma unroll
-    for (int i = 0; i < DH / 16; ++i)
-      qreg[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(
-          qp + (F8 ? 32 * (i / 2) + 16 * hf + 8 * (i % 2) : 16 * i + 8 * hf)));
+    for (int i = 0; i < NT; ++i)
+      qreg[nq][i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(
+          qp + (F8 && !HALF ? 64 * (i / 2) + 16 * qd + 8 * (i % 2) : 32 * i + 8 * qd)));
   }
   const int32_t* table = a.s.table + (long long)t.b * a.s.max_pages;
   auto tile_of = [&](int u) { return u < t.ts ? u : t.tw + (u - t.ts); };
+  // lanes l and l + 32 look up key l of a tile
   struct Look { int key, id, rem; };
   auto look = [&](int u) __attribute__((always_inline)) -> Look {
     Look k;
-    k.key = tile_of(min(u, t.nt - 1)) * TK + l32;
+    k.key = tile_of(min(u, t.nt - 1)) * TK + (lane & 31);
     const int kk = min(k.key, t.len - 1);
     const int pg = div_by(kk, a.s.page);
     k.id = table[pg];
     k.rem = kk - pg * a.page;
     return k;
   };
-  const long long row_bytes = (long long)a.H * DH * (F8 ? 1 : 2), head_bytes = (long long)h * DH * (F8 ? 1 : 2);
-  u32x4 kr[NK], vr[NV];
-  int ex = 0;
-  auto load_k = [&](int slot) __attribute__((always_inline)) {
-    const uint8_t* p = a.k + (long long)slot * row_bytes + head_bytes + 16 * hf;
+  const long long row_bytes = (long long)a.H * DH * (F8 ? 1 : 2);
+  const int lane_bytes = h * DH * (F8 ? 1 : 2) + qd * (HALF ? 8 : 16);
+  u32x4 kr[2][NL], vr[2][NL];
+  int ke[2], ve[2], ve_cur[2];
+  auto load_rows = [&](const uint8_t* base, const long long (&at)[2], u32x4 (&to)[2][NL]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) kr[i] = *reinterpret_cast<const u32x4*>(p + 32 * i);
-  };
-  auto load_v = [&](int slot) __attribute__((always_inline)) {
+    for (int r = 0; r < 2; ++r)
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int row = lane / CV + i * VSTEP;
-      vr[i] = *reinterpret_cast<const u32x4*>(a.v + (long long)__shfl(slot, row) * row_bytes + head_bytes + (lane % CV) * 16);
-    }
-  };
-  auto load_e = [&](int id) __attribute__((always_inline)) {
-    if constexpr (F8) {
-      const long long pe = (long long)(id >= 0 && id < a.pages ? id : 0) * a.H + h;
-      ex = (int)a.ke[pe] | (int)a.ve[pe] << 8;
-    }
+      for (int i = 0; i < NL; ++i) {
+        if constexpr (HALF) {
+          const u32x2 w = *reinterpret_cast<const u32x2*>(base + at[r]);
+          to[r][i] = u32x4{w.x, w.y, 0u, 0u};
+        } else {
+          to[r][i] = *reinterpret_cast<const u32x4*>(base + at[r] + 64 * i);
+        }
+      }
   };
   char* vt = smem + wave * (TK * ROWB);
-  auto store_v = [&](int e) __attribute__((always_inline)) {
+  auto vsw = [](int row) { return 2 * ((row / (16 / CPR)) & (CPR / 2 - 1)); };
+  // byte offsets in the value tile from which a lane writes and reads; their XORs with a
+  // chunk are formed again at each use (opaque() keeps them out of registers across the loop)
+  auto opaque = [](unsigned x) { asm volatile("" : "+v"(x)); return x; };
+  const unsigned vwr = (unsigned)(l16 * ROWB);
+  auto store_v = [&](unsigned wr) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int row = lane / CV + i * VSTEP;
-      char* at = vt + row * ROWB;
-      if constexpr (F8) {
-        const float sc = byte_scale(__shfl(e, row) >> 8);
-        const int ch = 2 * (lane % CV);
-        *reinterpret_cast<u32x4*>(at + ((ch ^ vswz(row, CPR)) * 16)) = widen8(vr[i].x, vr[i].y, sc);
-        *reinterpret_cast<u32x4*>(at + (((ch + 1) ^ vswz(row, CPR)) * 16)) = widen8(vr[i].z, vr[i].w, sc);
-      } else {
-        *reinterpret_cast<u32x4*>(at + (((lane % CV) ^ vswz(row, CPR)) * 16)) = vr[i];
+    for (int r = 0; r < 2; ++r) {
+      char* at = vt + wr + 16 * r * ROWB;      // rows l16 and l16 + 16 have the same swizzle
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const u32x4 w = vr[r][i];
+        if constexpr (HALF) {
+          *reinterpret_cast<u32x4*>(at + ((qd ^ vsw(l16)) * 16)) = widen8(w.x, w.y, byte_scale(ve_cur[r]));
+        } else if constexpr (F8) {
+          const float sc = byte_scale(ve_cur[r]);
+          const int ch = 8 * i + 2 * qd;
+          *reinterpret_cast<u32x4*>(at + ((ch ^ vsw(l16)) * 16)) = widen8(w.x, w.y, sc);
+          *reinterpret_cast<u32x4*>(at + (((ch + 1) ^ vsw(l16)) * 16)) = widen8(w.z, w.w, sc);
+        } else {
+          *reinterpret_cast<u32x4*>(at + (((4 * i + qd) ^ vsw(l16)) * 16)) = w;
+        }
       }
     }
   };
-  unsigned vbase;
-  {
-    const int gq = lane >> 4, la = lane & 15;
-    const int row = 4 * (gq >> 1) + (la >> 2);
-    const int c = 2 * (gq & 1) + ((la & 3) >> 1);
-    vbase = (unsigned)(row * ROWB + ((c ^ vswz(row, CPR)) * 16) + 8 * (la & 1));
-  }
-  auto read_v = [&](int db, int, int s2) __attribute__((always_inline)) -> bf16x8 {
-    const lds_char* p = (const lds_char*)(vt) + (vbase ^ (64u * db)) + 16 * s2 * ROWB;
+  // V^T operand of channels 16 db + l16, keys 16 (i / 4) + 4 qd + i % 4: the order in which
+  // S^T leaves them.  Of 16 lanes lane x reads row x / 4 and 4 channels from 4 (x % 4) on.
+  const int tr = 4 * qd + (l16 >> 2), trc = (l16 & 3) >> 1;
+  const unsigned vrd0 = (unsigned)(tr * ROWB + (trc ^ vsw(tr)) * 16 + 8 * (l16 & 1));
+  auto read_v = [&](unsigned rd, int db) __attribute__((always_inline)) -> bf16x8 {
+    const lds_char* p = (const lds_char*)(vt) + (rd ^ (32u * db));
+    // rows tr and tr + 16 have the same swizzle
     const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
-    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * ROWB)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * ROWB)));
     return __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
   };
 
-  f32x16 acc[ND];
+  f32x4 acc[NQ][ND];
+  float m_run[NQ], l_run[NQ];
 #pragma unroll
-  for (int db = 0; db < ND; ++db)
+  for (int nq = 0; nq < NQ; ++nq) {
+    m_run[nq] = kNoMax;
+    l_run[nq] = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[db][e] = 0.0f;
-  float m_run = kNoMax, l_run = 0.0f;
+    for (int db = 0; db < ND; ++db) acc[nq][db] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
 
-  auto resolve = [&](const Look& k, unsigned long long& there) __attribute__((always_inline)) -> int {
-    const bool in = k.id >= 0 && k.id < a.pages;
-    there = __ballot(in && k.key < t.len) & 0xffffffffull;
-    return in ? k.id * a.page + k.rem : 0;
-  };
   unsigned long long there = 0, there_next = 0;
+  long long at[2];
+  // places of the lane's two rows (row 0 of page 0 for keys that do not exist)
+  auto resolve = [&](const Look& k, unsigned long long& th) __attribute__((always_inline)) {
+    const bool in = k.id >= 0 && k.id < a.pages;
+    th = __ballot(in && k.key < t.len) & 0xffffffffull;
+    const int id = in ? k.id : 0, slot = in ? k.id * a.page + k.rem : 0;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      at[r] = (long long)__shfl(slot, l16 + 16 * r) * row_bytes + lane_bytes;
+      if constexpr (F8) {
+        const long long pe = (long long)__shfl(id, l16 + 16 * r) * a.H + h;
+        ke[r] = a.ke[pe];
+        ve[r] = a.ve[pe];
+      }
+    }
+  };
   Look nxt{};
   int u = u0 + wave;
   if (u < u1) {
     const Look first = look(u);
-    const int slot = resolve(first, there);
-    load_e(first.id);
-    load_k(slot);
-    load_v(slot);
+    resolve(first, there);
+    load_rows(a.k, at, kr);
+    load_rows(a.v, at, vr);
     nxt = look(u + W);
   }
 #pragma unroll 1
   for (; u < u1; u += W) {
     const bool more = u + W < u1;
     const int j0 = tile_of(u) * TK;
-    const int e_cur = ex;
-    f32x16 sn[1];
+    f32x4 sn[NQ][2];
 #pragma unroll
-    for (int i = 0; i < DH / 16; ++i) {
-      bf16x8 op;
-      if constexpr (F8) {
-        const u32x4 w = kr[i / 2];
-        const float sc = byte_scale(e_cur & 255);
-        op = __builtin_bit_cast(bf16x8, i % 2 == 0 ? widen8(w.x, w.y, sc) : widen8(w.z, w.w, sc));
-      } else {
-        op = __builtin_bit_cast(bf16x8, kr[i]);
+    for (int r = 0; r < 2; ++r) {
+      float sc = 0.0f;
+      if constexpr (F8) sc = byte_scale(ke[r]);
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        bf16x8 op;
+        if constexpr (F8) {
+          const u32x4 w = kr[r][i / 2];
+          op = __builtin_bit_cast(bf16x8, i % 2 == 0 ? widen8(w.x, w.y, sc) : widen8(w.z, w.w, sc));
+        } else {
+          op = __builtin_bit_cast(bf16x8, kr[r][i]);
+        }
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) sn[nq][r] = mfma16(op, qreg[nq][i], i == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sn[nq][r]);
       }
-      sn[0] = mfma(op, qreg[i], i == 0 ? f32x16{} : sn[0]);
     }
-    int slot = 0;
+    if constexpr (F8) {
+      ve_cur[0] = ve[0];
+      ve_cur[1] = ve[1];
+    }
     if (more) {
-      slot = resolve(nxt, there_next);
-      load_e(nxt.id);
-      load_k(slot);
+      resolve(nxt, there_next);
+      load_rows(a.k, at, kr);
       nxt = look(u + 2 * W);
     }
-    store_v(e_cur);
-    if (more) load_v(slot);
+    store_v(opaque(vwr));
+    const unsigned vrd = opaque(vrd0);
     const int kind = tile_kind<TK>(a, j0, p0, p1, there);
+    bool special = false;
+    if (kind == 1) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int db = 0; db < ND; ++db) m |= special_bits(read_v(vrd, db));
+      special = __ballot((m & 0x80008000u) != 0) != 0ull;
+    }
+    // (special tiles fetch the next values later: together with them they need more registers)
+    if (more && !special) load_rows(a.v, at, vr);
     if (kind != 0) {
-      if (kind == 1) mask_scores<1>(sn, j0, hf, lim, a.sinks, there);
-      bf16x8 pp[1][2];
-      softmax<1, ND>(sn, pp, m_run, l_run, acc, a.sl2);
-      if (kind == 2) values<1, ND>(read_v, pp, acc);
-      else values_masked<1, ND>(read_v, pp, acc);
+      if (kind == 1) {
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+          const uint32_t bits = visible_bits(lim[nq], a.sinks, j0, (uint32_t)there) >> (4 * qd);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (((bits >> (16 * (e / 4) + e % 4)) & 1) == 0) sn[nq][e / 4][e % 4] = -INFINITY;
+        }
+      }
+      bf16x8 pp[NQ];
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        // (see softmax)
+        float pe[8];
+        auto exps = [&]() __attribute__((always_inline)) -> float {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pe[e] = __builtin_amdgcn_exp2f(fmaf(sn[nq][e / 4][e % 4], a.sl2, -m_run[nq]));
+          return ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
+        };
+        float sum = exps();
+        if (__ballot(!(sum <= 256.0f)) != 0ull) {
+          float pm = sn[nq][0][0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) pm = fmaxf(pm, sn[nq][e / 4][e % 4]);
+          const float cand = fmaxf(m_run[nq], quarter_max(pm) * a.sl2);
+          const bool up = cand > m_run[nq] + kMaxSlack;
+          const float m_new = up ? cand : m_run[nq];
+          const float corr = __builtin_amdgcn_exp2f(m_run[nq] - m_new);
+          l_run[nq] *= corr;
+          m_run[nq] = m_new;
+#pragma unroll
+          for (int db = 0; db < ND; ++db) acc[nq][db] *= corr;
+          sum = exps();
+        }
+        pp[nq] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(pe[0], pe[1]), pack_bf16x2(pe[2], pe[3]),
+                                                  pack_bf16x2(pe[4], pe[5]), pack_bf16x2(pe[6], pe[7])});
+        l_run[nq] += sum;
+      }
+      if (!special) {
+#pragma unroll
+        for (int db = 0; db < ND; ++db) {
+          const bf16x8 op = read_v(vrd, db);
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq) acc[nq][db] = mfma16(op, pp[nq], acc[nq][db]);
+        }
+      } else {
+#pragma unroll
+        for (int db = 0; db < ND; ++db) {
+          const Images v = images(read_v(vrd, db));
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq) {
+            const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+            const bf16x8 w = seen_weights(pp[nq]);
+            acc[nq][db] = mfma16(v.fin, pp[nq], acc[nq][db]);
+            add_special<4>(acc[nq][db], mfma16(v.pos, w, zero), mfma16(v.neg, w, zero));
+          }
+        }
+        if (more) load_rows(a.v, at, vr);
+      }
     }
     there = there_next;
   }
 
   // ---- join the four waves: weights 2^(m_w - max m)
-  const float l = l_run + __shfl_xor(l_run, 32);
-  if (hf == 0) {
-    sm[wave][l32] = m_run;
-    sl[wave][l32] = l;
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    float l = l_run[nq] + __shfl_xor(l_run[nq], 16);
+    l += __shfl_xor(l, 32);
+    if (qd == 0) {
+      sm[wave][16 * nq + l16] = m_run[nq];
+      sl[wave][16 * nq + l16] = l;
+    }
   }
   __syncthreads();
-  float* part = reinterpret_cast<float*>(smem) + wave * kRows * DH;
-  if (l32 < nrows) {
+  float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
-    for (int db = 0; db < ND; ++db)
+  for (int nq = 0; nq < NQ; ++nq)
+    if (16 * nq + l16 < nrows) {
 #pragma unroll
-      for (int g4 = 0; g4 < 4; ++g4)
-        *reinterpret_cast<f32x4*>(part + l32 * DH + db * 32 + 8 * g4 + 4 * hf) =
-            f32x4{acc[db][4 * g4], acc[db][4 * g4 + 1], acc[db][4 * g4 + 2], acc[db][4 * g4 + 3]};
-  }
+      for (int db = 0; db < ND; ++db)
+        *reinterpret_cast<f32x4*>(part + (wave * TM + 16 * nq + l16) * DH + 16 * db + 4 * qd) = acc[nq][db];
+    }
   __syncthreads();
+  const long long item = blockIdx.x;
+  if (a.target > 0 && it.z == 0 && tid == 0) a.meta[(long long)it.tile_id * a.H + h] = make_int2(it.item0, it.pieces);
   for (int i = tid; i < nrows * (DH / 4); i += kThreads) {
     const int ql = i / (DH / 4), d = 4 * (i % (DH / 4));
     float m = sm[0][ql];
@@ -710,21 +934,60 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttnArgs a) {
       if (sl[w][ql] == 0.0f) continue;         // saw no key
       const float c = __builtin_amdgcn_exp2f(sm[w][ql] - m);
       lt += c * sl[w][ql];
-      o += c * *reinterpret_cast<const f32x4*>(reinterpret_cast<float*>(smem) + (w * kRows + ql) * DH + d);
+      o += c * *reinterpret_cast<const f32x4*>(part + (w * TM + ql) * DH + d);
     }
     const bool some = lt != 0.0f;              // true for NaN, too
     o *= some ? 1.0f / lt : 0.0f;
     const float l2 = some ? m + __log2f(lt) : -INFINITY;
-    const int rr = t.row0 + ql, tk = rr / a.g;
-    const long long row = (long long)(t.beg + tk) * a.Hq + h * a.g + (rr - tk * a.g);
-    if (a.npieces > 1) {
-      const long long at = (long long)blockIdx.z * a.s.n_tok * a.Hq + row;
-      *reinterpret_cast<f32x4*>(a.part_o + at * DH + d) = o;
-      if (d == 0) a.part_lse[at] = l2;
+    if (it.pieces > 1) {
+      *reinterpret_cast<f32x4*>(a.part_o + (item * TM + ql) * DH + d) = o;
+      if (d == 0) a.part_lse[item * TM + ql] = l2;
     } else {
+      const int rr = t.row0 + ql, tk = rr / a.g;
+      const long long row = (long long)(t.beg + tk) * a.Hq + h * a.g + (rr - tk * a.g);
       put4(a, row, DH, d, o);
       if (a.lse != nullptr && d == 0) a.lse[row] = l2 * kLn2;
     }
+  }
+}
+
+// Join of the pieces of a row tile that the rows kernel cut: with l_z the log2 log-sum-exp
+// and O_z the normalised output of piece z, O = sum 2^(l_z - max) O_z / sum 2^(l_z - max).
+// Pieces without a visible key (-inf) add nothing.
+template <int DH, int TM>
+__global__ __launch_bounds__(kThreads) void kv_rows_join_kernel(KvAttnArgs a) {
+  RowTile t;
+  if (!row_tile<TM, kRowKeys>(a, blockIdx.x, t)) return;
+  const int2 meta = a.meta[(long long)blockIdx.x * a.H + blockIdx.y];
+  // (the bounds hold for whatever lies in the workspace)
+  if (meta.y < 2 || meta.x < 0 || meta.x >= a.max_items || meta.y > (a.max_items - 1 - meta.x) / a.H + 1) return;
+  const int nrows = min(TM, t.n_rows - t.row0);
+  for (int i = threadIdx.x; i < nrows * (DH / 4); i += kThreads) {
+    const int ql = i / (DH / 4), d = 4 * (i % (DH / 4));
+    auto lse_of = [&](int z) { return a.part_lse[(long long)(meta.x + z * a.H) * TM + ql]; };
+    float m = -INFINITY;
+    for (int z = 0; z < meta.y; ++z) {
+      const float l = lse_of(z);
+      m = l > m || l != l ? l : m;
+    }
+    float w = 0.0f;
+    f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int z = 0; z < meta.y; ++z) {
+      const float l = lse_of(z);
+      const f32x4 p = *reinterpret_cast<const f32x4*>(a.part_o + ((long long)(meta.x + z * a.H) * TM + ql) * DH + d);
+      const float c = l == m ? 1.0f : __builtin_amdgcn_exp2f(l - m);
+      if (l != -INFINITY) {
+        w += c;
+        o += c * p;
+      }
+    }
+    const bool some = w != 0.0f;
+    o *= some ? 1.0f / w : 0.0f;
+    const int rr = t.row0 + ql, tk = rr / a.g;
+    const long long row = (long long)(t.beg + tk) * a.Hq + blockIdx.y * a.g + (rr - tk * a.g);
+    put4(a, row, DH, d, o);
+    if (a.lse != nullptr && d == 0) a.lse[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
   }
 }
 
@@ -760,11 +1023,19 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(KvAttnArgs a) {
   if (a.lse != nullptr && d == 0) a.lse[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
 }
 
+template <int DH, bool F8, int NQ>
+void launch_rows(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
+  const int items = p.target > 0 ? p.max_items : p.row_tiles * a.H;
+  hipLaunchKernelGGL((kv_rows_kernel<DH, F8, NQ>), dim3(items), dim3(kThreads), 0, stream, a);
+  if (p.target > 0)
+    hipLaunchKernelGGL((kv_rows_join_kernel<DH, 16 * NQ>), dim3(p.row_tiles, a.H), dim3(kThreads), 0, stream, a);
+}
+
 template <int DH, bool F8>
 void launch_as(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
-  const dim3 grid(p.row_tiles, a.H, p.pieces);
-  if (p.few_rows) hipLaunchKernelGGL((kv_rows_kernel<DH, F8>), grid, dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((kv_tiles_kernel<DH, F8>), grid, dim3(kThreads), 0, stream, a);
+  if (p.rows == 16) return launch_rows<DH, F8, 1>(a, p, stream);
+  if (p.rows == 32) return launch_rows<DH, F8, 2>(a, p, stream);
+  hipLaunchKernelGGL((kv_tiles_kernel<DH, F8>), dim3(p.row_tiles, a.H, p.pieces), dim3(kThreads), 0, stream, a);
   if (p.pieces > 1) {
     const long long threads = (long long)a.s.n_tok * a.Hq * (DH / 4);
     hipLaunchKernelGGL((kv_join_kernel<DH>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
@@ -778,24 +1049,35 @@ KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, long l
                         int cus) {
   KvAttnPlan p{};
   const long long rows = n_tok * g, mean = (rows + n_seq - 1) / n_seq;
-  p.few_rows = mean <= 2 * kRows;
-  const int tm = p.few_rows ? kRows : kTileRows, tk = p.few_rows ? kRowKeys : kTileKeys;
-  p.row_tiles = (int)(rows / tm + n_seq);
+  p.rows = mean <= 16 ? 16 : mean <= 64 ? 32 : kTileRows;
+  const int tk = p.rows == kTileRows ? kTileKeys : kRowKeys;
+  p.row_tiles = (int)(rows / p.rows + n_seq);
   p.pieces = 1;
   p.piece_tiles = 1;
   if (cus <= 0 || n_tok < 1) return p;
-  const long long units = (long long)n_seq * ((mean + tm - 1) / tm) * H;
+  const long long units = (long long)n_seq * ((mean + p.rows - 1) / p.rows) * H;
   long long keys = max_len;
   if (window > 0) keys = std::min(keys, (long long)window + (mean + g - 1) / g + sinks + 2 * tk);
   const long long nt = (keys + tk - 1) / tk;
-  const long long least = p.few_rows ? 16 : 8;       // key tiles of a piece
-  const long long want = (long long)cus * (p.few_rows ? 8 : 2) / std::max(units, 1ll);
-  const long long most = std::min<long long>(std::min<long long>(want, kMaxPieces), (nt + least - 1) / least);
+  if (p.rows < kTileRows) {
+    // workgroups resident at once, less the partial pieces that the row tiles end with
+    const long long resident = (long long)cus * (p.rows == 16 ? 3 : 2);
+    if (nt <= kMinPiece || units >= resident) return p;
+    p.target = (int)std::max(resident - units / 2, resident / 2);
+    p.max_items = p.target + p.row_tiles * H + 1;
+    p.part_bytes = align_up((size_t)p.max_items * p.rows * dh * 4);
+    p.lse_bytes = align_up((size_t)p.max_items * p.rows * 4);
+    p.bytes = p.part_bytes + p.lse_bytes + align_up((size_t)p.row_tiles * H * sizeof(int2));
+    return p;
+  }
+  const long long want = (long long)cus * 2 / std::max(units, 1ll);
+  const long long most = std::min<long long>(std::min<long long>(want, kMaxPieces), (nt + 7) / 8);   // 8 key tiles at least
   if (most < 2) return p;
   p.piece_tiles = (int)((nt + most - 1) / most);
   p.pieces = (int)((nt + p.piece_tiles - 1) / p.piece_tiles);
   p.part_bytes = align_up((size_t)most * n_tok * H * g * dh * 4);
-  p.bytes = p.part_bytes + align_up((size_t)most * n_tok * H * g * 4);
+  p.lse_bytes = align_up((size_t)most * n_tok * H * g * 4);
+  p.bytes = p.part_bytes + p.lse_bytes;
   return p;
 }
 
@@ -813,7 +1095,10 @@ cast_status_t launch_kv_attn(const void* q, long long q_stride, int Hq, const ca
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
   a.part_o = static_cast<float*>(workspace);
-  a.part_lse = plan.pieces > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.part_bytes) : nullptr;
+  a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.part_bytes);
+  a.meta = reinterpret_cast<int2*>(static_cast<char*>(workspace) + plan.part_bytes + plan.lse_bytes);
+  a.target = plan.target;
+  a.max_items = plan.max_items;
   a.Hq = Hq;
   a.H = c.H;
   a.g = Hq / c.H;
