@@ -88,6 +88,7 @@ class KvSeqsStruct(ctypes.Structure):
 
 
 _lib = None
+_torch = None                     # set by load()
 _c = ctypes
 _ll = _c.c_longlong
 _vp, _i, _f, _sz = _c.c_void_p, _c.c_int, _c.c_float, _c.c_size_t
@@ -98,7 +99,9 @@ def load(path: str = LIB_PATH):
     global _lib
     if _lib is not None:
         return _lib
-    import torch  # noqa: F401  (loads the HIP runtime libcast.so must share)
+    import torch  # (loads the HIP runtime libcast.so must share)
+    global _torch
+    _torch = torch
     if not os.path.exists(path):
         raise RuntimeError(f"{path} is not built; run python -m paper_2609_34144_amd.build")
     lib = ctypes.CDLL(path, mode=ctypes.RTLD_LOCAL)
@@ -506,25 +509,36 @@ def _want(name: str, t, dtypes, device=None, dense: bool = True):
     return t
 
 
-def _rows(name: str, t, heads, dh, n, device):
+def _rows(name, t, heads, dh, n, device):
     """Token stride of bf16 [n, heads, dh] with dense heads."""
-    import torch
-    _want(name, t, (torch.bfloat16,), device, dense=False)
-    if t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or t.shape[2] != dh:
+    if t.dtype != _torch.bfloat16:
+        _bad(f"{name} must be torch.bfloat16, got {t.dtype}")
+    if t.device != device:
+        _bad(f"{name} is on {t.device}, expected {device}")
+    if t.shape != (n, heads, dh):
         _bad(f"{name} must be [{n}, {heads}, {dh}], got {list(t.shape)}")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dh):
+    s = t.stride()
+    if s[2] != 1 or (s[1] != dh and heads > 1):
         _bad(f"{name} must have dense heads")
-    return t.stride(0) if n > 1 else heads * dh
+    return s[0] if n > 1 else heads * dh
+
+
+def _same(name, t, like, dtype):
+    """A dense output of the shape and device of `like`."""
+    if t.dtype != dtype or t.shape != like.shape or t.device != like.device or not t.is_contiguous():
+        _bad(f"{name} must be a contiguous {dtype} {list(like.shape)} on {like.device}, got {t.dtype} "
+             f"{list(t.shape)} on {t.device}")
 
 
 def _on(device, stream):
-    """The stream's handle, after checking that `device` is current (kernels run there)."""
-    import torch
-    if device.type != "cuda":
+    """The stream's handle, after checking that `device` is current (kernels run there).  Small
+    calls are bound by the host, so this takes torch's raw handle rather than a Stream object."""
+    index = device.index
+    if index is None or device.type != "cuda":
         _bad(f"tensors must be on a GPU, got {device}")
-    if device.index != torch.cuda.current_device():
-        _bad(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    return _stream(stream)
+    if index != _torch.cuda.current_device():
+        _bad(f"tensors are on {device}, the current device is cuda:{_torch.cuda.current_device()}")
+    return _torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
 
 
 def cast_rope_frequencies(axis_dims, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -579,10 +593,11 @@ def cast_rope_params_init(rot_dim: int, base: float = 10000.0, interleaved: bool
 
 
 def _pos(pos, n, rope, device):
-    import torch
-    _want("pos", pos, (torch.int32,), device)
-    if pos.numel() != n * rope.n_axes or pos.shape[0] != n:
-        _bad(f"pos must be [{n}, {rope.n_axes}], got {list(pos.shape)}")
+    if pos.dtype != _torch.int32 or pos.device != device or not pos.is_contiguous():
+        _bad(f"pos must be a contiguous torch.int32 tensor on {device}, got {pos.dtype} on {pos.device}")
+    shape = pos.shape
+    if shape != (n, rope.n_axes) and (rope.n_axes != 1 or shape != (n,)):
+        _bad(f"pos must be [{n}, {rope.n_axes}], got {list(shape)}")
     return pos.data_ptr()
 
 
@@ -590,26 +605,32 @@ def cast_rope(x, pos, rope: RopeParams, transpose: bool = False, out=None, strea
     """Rotary positions.  x [n, H, dh] fp32 or bf16 (device, any token and head strides); pos
     int32 [n, n_axes] (or [n]).  `out` may be x itself.  transpose: turn the other way (the
     gradient of the rotation).  Returns out."""
-    import torch
-    lib = load()
-    _want("x", x, (torch.float32, torch.bfloat16), dense=False)
-    if x.dim() != 3:
-        _bad(f"x must be [n, H, dh], got {list(x.shape)}")
-    n, H, dh = x.shape
+    lib = _lib or load()
+    dtype, device, shape, xs = x.dtype, x.device, x.shape, x.stride()
+    if dtype != _torch.bfloat16 and dtype != _torch.float32:
+        _bad(f"x must be torch.float32 or torch.bfloat16, got {dtype}")
+    if len(shape) != 3:
+        _bad(f"x must be [n, H, dh], got {list(shape)}")
+    n, H, dh = shape
     if out is None:
-        out = torch.empty((n, H, dh), dtype=x.dtype, device=x.device)
-    _want("out", out, (x.dtype,), x.device, dense=False)
-    if out.shape != x.shape:
-        _bad(f"out must be {list(x.shape)}, got {list(out.shape)}")
-    if (x.stride(2) != 1 or out.stride(2) != 1) and n > 0:
+        out = _torch.empty_like(x, memory_format=_torch.contiguous_format)
+        os_ = (H * dh, dh, 1)
+    else:
+        if out.dtype != dtype or out.device != device or out.shape != shape:
+            _bad(f"out must be {dtype} {list(shape)} on {device}, got {out.dtype} {list(out.shape)} on {out.device}")
+        os_ = out.stride()
+    if (xs[2] != 1 or os_[2] != 1) and n > 0:
         _bad("the channels of x and out must be dense")
-    if rope.device != x.device:
-        _bad(f"the rotation's tables are on {rope.device}, x on {x.device}")
-    pp = _pos(pos, n, rope, x.device)
-    st = lambda t: (t.stride(0) if n > 1 else max(t.stride(0), H * dh), t.stride(1) if H > 1 else dh)  # noqa: E731
-    xs, os_ = st(x), st(out)
-    _check(lib.cast_rope(x.data_ptr(), 0 if x.dtype == torch.float32 else 1, n, H, dh, xs[0], xs[1], pp, rope.ref,
-                         int(bool(transpose)), out.data_ptr(), os_[0], os_[1], _on(x.device, stream)))
+    if rope.device != device:
+        _bad(f"the rotation's tables are on {rope.device}, x on {device}")
+    if n < 2 or H < 2:                                 # torch gives any stride to a dimension of one
+        fix = lambda s: (s[0] if n > 1 else max(s[0], H * dh), s[1] if H > 1 else dh)  # noqa: E731
+        xs, os_ = fix(xs), fix(os_)
+    pp = _pos(pos, n, rope, device)
+    st = lib.cast_rope(x.data_ptr(), 1 if dtype == _torch.bfloat16 else 0, n, H, dh, xs[0], xs[1], pp, rope.ref,
+                       1 if transpose else 0, out.data_ptr(), os_[0], os_[1], _on(device, stream))
+    if st:
+        _check(st)
     return out
 
 
@@ -667,6 +688,7 @@ class KvSeqs:
             _bad(f"need cu [n_seq + 1], lens [n_seq], table [n_seq, max_pages], got {list(cu.shape)}, "
                  f"{list(lens.shape)}, {list(table.shape)}")
         self.cu, self.lens, self.table, self.device = cu, lens, table, cu.device
+        self.max_pages = table.shape[1]
         self._structs = {}
 
     def ref(self, n_tok: int):
@@ -680,38 +702,38 @@ class KvSeqs:
         return r
 
 
-def _same_device(cache, seqs):
-    if seqs.device != cache.device:
-        _bad(f"the sequences are on {seqs.device}, the cache on {cache.device}")
-
-
 def cast_kv_append(cache: KvCache, seqs: KvSeqs, k, v, rope: RopeParams | None = None, pos=None, q=None,
                    q_out=None, stream=None):
     """Store k, v (bf16 [n, H, dh], heads dense, any token stride) into the cache's pages, keys
     rotated by `rope` (None: as they come) at pos (int32 [n, n_axes]; None: the token's index in
     its sequence), and rotate the queries q [n, Hq, dh].  Returns q_out, or None without q."""
-    import torch
-    lib = load()
-    n, dev = k.shape[0], cache.device
-    _same_device(cache, seqs)
-    ks, vs = _rows("k", k, cache.H, cache.dh, n, dev), _rows("v", v, cache.H, cache.dh, n, dev)
-    qs, hq = 0, 0
+    lib = _lib or load()
+    n, dev, H, dh = k.shape[0], cache.device, cache.H, cache.dh
+    if seqs.device != dev:
+        _bad(f"the sequences are on {seqs.device}, the cache on {dev}")
+    ks, vs = _rows("k", k, H, dh, n, dev), _rows("v", v, H, dh, n, dev)
+    qs = hq = 0
+    qp = op = rp = pp = None
     if q is not None:
         hq = q.shape[1] if q.dim() == 3 else 0
-        qs = _rows("q", q, hq, cache.dh, n, dev)
+        qs = _rows("q", q, hq, dh, n, dev)
         if q_out is None:
-            q_out = torch.empty((n, hq, cache.dh), dtype=q.dtype, device=dev)
-        _want("q_out", q_out, (torch.bfloat16,), dev)
-        if q_out.shape != q.shape:
-            _bad(f"q_out must be {list(q.shape)}, got {list(q_out.shape)}")
-    if rope is not None and rope.device != dev:
-        _bad(f"the rotation's tables are on {rope.device}, the cache on {dev}")
-    if rope is None and pos is not None:
+            q_out = _torch.empty_like(q, memory_format=_torch.contiguous_format)
+        else:
+            _same("q_out", q_out, q, _torch.bfloat16)
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    if rope is not None:
+        if rope.device != dev:
+            _bad(f"the rotation's tables are on {rope.device}, the cache on {dev}")
+        rp = rope.ref
+        if pos is not None:
+            pp = _pos(pos, n, rope, dev)
+    elif pos is not None:
         _bad("pos is given without a rotation")
-    pp = None if pos is None else _pos(pos, n, rope, dev)
-    _check(lib.cast_kv_append(cache.ref, seqs.ref(n), k.data_ptr(), ks, v.data_ptr(), vs,
-                              None if rope is None else rope.ref, pp, _ptr(q), qs, hq,
-                              None if q is None else q_out.data_ptr(), _on(dev, stream)))
+    st = lib.cast_kv_append(cache.ref, seqs.ref(n), k.data_ptr(), ks, v.data_ptr(), vs, rp, pp, qp, qs, hq, op,
+                            _on(dev, stream))
+    if st:
+        _check(st)
     return None if q is None else q_out
 
 
@@ -719,24 +741,29 @@ def cast_kv_read(cache: KvCache, pages, k_out=None, v_out=None, want_k: bool = T
                  stream=None):
     """The pages `pages` (int32 [m], device) as bf16 history blocks (k, v) [m, page, H, dh], the
     layout of cast_route_kv and cast_anchor_attn; None where not wanted."""
-    import torch
-    lib = load()
-    _want("pages", pages, (torch.int32,), cache.device)
-    shape = (pages.numel(), cache.page, cache.H, cache.dh)
-    mk = lambda t, want: t if t is not None or not want else torch.empty(shape, dtype=torch.bfloat16, device=cache.device)  # noqa: E731
-    k_out, v_out = mk(k_out, want_k), mk(v_out, want_v)
+    lib = _lib or load()
+    dev = cache.device
+    if pages.dtype != _torch.int32 or pages.device != dev or not pages.is_contiguous():
+        _bad(f"pages must be a contiguous torch.int32 tensor on {dev}, got {pages.dtype} on {pages.device}")
+    m = pages.numel()
+    shape = (m, cache.page, cache.H, cache.dh)
     for name, t in (("k_out", k_out), ("v_out", v_out)):
         if t is not None:
-            _want(name, t, (torch.bfloat16,), cache.device)
-            if tuple(t.shape) != shape:
+            _want(name, t, (_torch.bfloat16,), dev)
+            if t.shape != shape:
                 _bad(f"{name} must be {list(shape)}, got {list(t.shape)}")
-    _check(lib.cast_kv_read(cache.ref, pages.data_ptr(), shape[0], _ptr(k_out), _ptr(v_out),
-                            _on(cache.device, stream)))
+    if k_out is None and want_k:
+        k_out = _torch.empty(shape, dtype=_torch.bfloat16, device=dev)
+    if v_out is None and want_v:
+        v_out = _torch.empty(shape, dtype=_torch.bfloat16, device=dev)
+    st = lib.cast_kv_read(cache.ref, pages.data_ptr(), m, _ptr(k_out), _ptr(v_out), _on(dev, stream))
+    if st:
+        _check(st)
     return k_out, v_out
 
 
 def _max_len(cache, seqs, max_len):
-    top = seqs.table.shape[1] * cache.page
+    top = seqs.max_pages * cache.page
     return top if max_len is None else max(1, min(int(max_len), top))
 
 
@@ -753,35 +780,42 @@ def cast_kv_attn(q, cache: KvCache, seqs: KvSeqs, scale: float, causal: bool = T
     returns (out bf16 [n, Hq, dh], lse fp32 [n, Hq] or None).  max_len: the longest length
     expected (default: what the table holds); split=True uses `workspace` (allocated here when
     None) to cut long key ranges into pieces, split=False runs every row tile whole."""
-    import torch
-    lib = load()
+    lib = _lib or load()
     if q.dim() != 3:
         _bad(f"q must be [n, Hq, dh], got {list(q.shape)}")
-    n, hq, dev = q.shape[0], q.shape[1], cache.device
-    _same_device(cache, seqs)
+    n, hq, dh = q.shape
+    dev = cache.device
+    if seqs.device != dev:
+        _bad(f"the sequences are on {seqs.device}, the cache on {dev}")
     qs = _rows("q", q, hq, cache.dh, n, dev)
     if out is None:
-        out = torch.empty((n, hq, cache.dh), dtype=torch.bfloat16, device=dev)
+        out = _torch.empty_like(q, memory_format=_torch.contiguous_format)
     else:
-        _want("out", out, (torch.bfloat16,), dev)
-        if out.shape != q.shape:
-            _bad(f"out must be {list(q.shape)}, got {list(out.shape)}")
-    if lse_out is None:
-        if want_lse:
-            lse_out = torch.empty((n, hq), dtype=torch.float32, device=dev)
-    else:
-        _want("lse_out", lse_out, (torch.float32,), dev)
-        if tuple(lse_out.shape) != (n, hq):
+        _same("out", out, q, _torch.bfloat16)
+    lp = None
+    if lse_out is not None:
+        _want("lse_out", lse_out, (_torch.float32,), dev)
+        if lse_out.shape != (n, hq):
             _bad(f"lse_out must be {[n, hq]}, got {list(lse_out.shape)}")
-    top, sref, causal = _max_len(cache, seqs, max_len), seqs.ref(n), int(bool(causal))
+        lp = lse_out.data_ptr()
+    elif want_lse:
+        lse_out = _torch.empty((n, hq), dtype=_torch.float32, device=dev)
+        lp = lse_out.data_ptr()
+    top, sref, causal = _max_len(cache, seqs, max_len), seqs.ref(n), 1 if causal else 0
     strm = _on(dev, stream)
     ws, wsb = None, 0
     if split:
         if workspace is not None:
-            _want("workspace", workspace, (workspace.dtype,), dev)
-            ws, wsb = workspace, workspace.numel() * workspace.element_size()
+            if workspace.device != dev or not workspace.is_contiguous():
+                _bad(f"the workspace must be a contiguous tensor on {dev}, got one on {workspace.device}")
+            ws, wsb = workspace.data_ptr(), workspace.nbytes
         else:
-            ws, wsb = _ws(lib.cast_kv_attn_workspace_bytes(cache.ref, sref, hq, top, causal, window, sinks), dev, None)
-    _check(lib.cast_kv_attn(q.data_ptr(), qs, hq, cache.ref, sref, top, causal, window, sinks, scale, out.data_ptr(),
-                            _ptr(lse_out), _ptr(ws), wsb, strm))
+            wsb = lib.cast_kv_attn_workspace_bytes(cache.ref, sref, hq, top, causal, window, sinks)
+            if wsb:
+                workspace = _torch.empty(wsb, dtype=_torch.uint8, device=dev)
+                ws = workspace.data_ptr()
+    st = lib.cast_kv_attn(q.data_ptr(), qs, hq, cache.ref, sref, top, causal, window, sinks, scale, out.data_ptr(), lp,
+                          ws, wsb, strm)
+    if st:
+        _check(st)
     return out, lse_out
