@@ -119,17 +119,22 @@ __device__ __forceinline__ void rotate_item(const T* x, T* y, int i, int mode, i
   }
 }
 
+// a (cos, sin) of a reduced angle.  v_cos and v_sin take revolutions; over [-0.5, 0.5] they
+// are off by at most 1.3e-7 (all multiples of 2^-24 against fp64), about one fp32 step of 1.
+__device__ __forceinline__ f32x2 cos_sin(float revs, float amp) {
+  return f32x2{__builtin_amdgcn_cosf(revs) * amp, __builtin_amdgcn_sinf(revs) * amp};
+}
+
 // (cos, sin) of the block's tokens' pairs into LDS: token of the block tt, position of axis
-// a given by pos_of(tt, a).  sincospif on the reduced angle: full fp32 precision.
+// a given by pos_of(tt, a).
 template <class F>
 __device__ __forceinline__ void fill_angles(f32x2 (*cs)[kMaxPairs], const Rope& r, F&& pos_of) {
   const int pairs = r.rot >> 1;
   for (int t = threadIdx.x; t < kTok * kMaxPairs; t += kThreads) {
     const int tt = t / kMaxPairs, j = t % kMaxPairs;
     if (j < pairs) {
-      float s, c;
-      sincospif(2.0f * rope_revs(r.turns[j], pos_of(tt, rope_axis(r, j))), &s, &c);
-      cs[tt][j] = f32x2{c * r.amp, s * r.amp * r.sign};
+      const f32x2 c = cos_sin(rope_revs(r.turns[j], pos_of(tt, rope_axis(r, j))), r.amp);
+      cs[tt][j] = f32x2{c.x, c.y * r.sign};
     }
   }
 }
@@ -262,11 +267,11 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
 // ---------------------------------------------------------------------------
 // cast_kv_append, e4m3 cache
 // ---------------------------------------------------------------------------
-// v as an e4m3 code (nearest even) under 1/scale `inv`; two per call.  The unit saturates
-// nothing here: |v * inv| <= 448 for finite v.
-__device__ __forceinline__ uint32_t code1(float v, float inv) {
-  const uint32_t c = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v * inv, 0.0f, 0, false) & 0xffu;
-  return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? 0x7fu : c;
+// Four values as e4m3 codes (nearest even) under 1/scale `inv`: |v * inv| <= 448 for finite
+// v, infinities and NaN become NaN.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
 }
 __device__ __forceinline__ float exp_scale(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
@@ -278,61 +283,166 @@ __device__ __forceinline__ int need_exp(float top) {
   return max(e - 9 + (m > 0.875f ? 1 : 0), -117);
 }
 
-// Eight channels [8c, 8c + 8) of one head's row, rotated (or not) in registers; the angles
-// are formed on the spot, v_sin and v_cos taking revolutions (their error, 2^-20 or so, is far
-// below the 2^-4 of the codes).
-__device__ __forceinline__ void rotated8(const uint16_t* x, int c, const Rope& r, long long pos_row,
-                                         int index, float* y) {
-  load8(x + 8 * c, y);
-  if (8 * c >= r.rot) return;
-  auto turn = [&](int j) -> f32x2 {
-    const int p = r.pos != nullptr ? r.pos[pos_row * r.n_axes + rope_axis(r, j)] : index;
-    const float f = rope_revs(r.turns[j], p);
-    return f32x2{__builtin_amdgcn_cosf(f) * r.amp, __builtin_amdgcn_sinf(f) * r.amp};
-  };
-  if (r.inter) {
+__device__ __forceinline__ void unpack8(u32x4 w, float* f) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (8 * c + 2 * e < r.rot) {
-        const f32x2 t = turn(4 * c + e);
-        const float u = y[2 * e], w = y[2 * e + 1];
-        y[2 * e] = fmaf(u, t.x, -(w * t.y));
-        y[2 * e + 1] = fmaf(u, t.y, w * t.x);
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = bf16lo(w[i]);
+    f[2 * i + 1] = bf16hi(w[i]);
+  }
+}
+
+// The new rows of one (page, head, K or V): the largest magnitude gives the exponent, then
+// the codes are written.  An item is two chunks of eight channels; a thread keeps one item
+// of every `step`-th token, so the frequencies of its pairs are read once and an angle
+// serves both channels of its pair.
+//   MODE 0  no rotation: chunks 2 i and 2 i + 1
+//        1  half layout, rot a multiple of 16: items < rot/16 take chunks i and i + rot/16
+//        2  interleaved
+//        3  half layout, any rot: partners are read one by one
+// kKeep items are loaded together and stay in registers between the two passes; longer
+// pages are read again (from the L2).
+struct PageRows {
+  const uint16_t* src;           // the call's first row of the page, this head
+  long long ss;                  // its token stride
+  uint8_t* page;                 // row 0 of the page, this head
+  long long cs;                  // its row stride
+  uint8_t* exponent;
+  int had, n, row0, index0;      // earlier tokens, new ones; first call row and index in the sequence
+};
+constexpr int kKeep = 2;
+template <int MODE>
+__device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int dh, float* tops) {
+  const int ipr = dh >> 4, shift = 31 - __clz(ipr);            // items per row
+  const int item = threadIdx.x & (ipr - 1), t0 = threadIdx.x >> shift, step = kThreads >> shift;
+  const int half = r.rot >> 1;
+  int c0 = 16 * item, c1 = c0 + 8;               // first channels of the item's chunks
+  bool turns = MODE != 0 && c0 < r.rot;
+  if (MODE == 1) {
+    turns = item < (r.rot >> 4);
+    if (turns) {
+      c0 = 8 * item;
+      c1 = c0 + half;
+    }
+  }
+  constexpr int NF = MODE == 0 ? 1 : MODE == 3 ? 16 : 8;       // angles of an item
+  double freq[NF];
+  uint32_t axes = 0;                             // two bits each
+  if (MODE != 0 && turns) {
+#pragma unroll
+    for (int e = 0; e < NF; ++e) {
+      const int ch = c0 + e;
+      const int j = MODE == 1 ? ch : MODE == 2 ? (c0 >> 1) + e : ch >= half ? ch - half : ch;
+      const int jj = min(j, half - 1);
+      freq[e] = r.turns[jj];
+      axes |= (uint32_t)rope_axis(r, jj) << (2 * e);
+    }
+  }
+  auto fetch = [&](int base, float (&y)[kKeep][16]) __attribute__((always_inline)) {
+    u32x4 w[kKeep][2];
+#pragma unroll
+    for (int j = 0; j < kKeep; ++j) {
+      const uint16_t* row = g.src + min(base + t0 + j * step, g.n - 1) * g.ss;
+      w[j][0] = *reinterpret_cast<const u32x4*>(row + c0);
+      w[j][1] = *reinterpret_cast<const u32x4*>(row + c1);
+    }
+#pragma unroll
+    for (int j = 0; j < kKeep; ++j) {
+      unpack8(w[j][0], y[j]);
+      unpack8(w[j][1], y[j] + 8);
+      if (MODE == 0 || !turns) continue;
+      const int t = min(base + t0 + j * step, g.n - 1);
+      const int32_t* pos = r.pos != nullptr ? r.pos + (long long)(g.row0 + t) * r.n_axes : nullptr;
+      const int p0 = pos != nullptr ? pos[0] : g.index0 + t;
+      auto angle = [&](int e) {
+        return cos_sin(rope_revs(freq[e], r.n_axes > 1 && pos != nullptr ? pos[(axes >> (2 * e)) & 3] : p0), r.amp);
+      };
+      const uint16_t* row = g.src + t * g.ss;
+#pragma unroll
+      for (int e = 0; e < NF; ++e) {
+        if (MODE == 3) {
+          const int ch = c0 + e;
+          if (ch < r.rot) {
+            const f32x2 a = angle(e);
+            const float o = to_f32(row[ch < half ? ch + half : ch - half]);
+            y[j][e] = fmaf(y[j][e], a.x, ch < half ? -(o * a.y) : o * a.y);
+          }
+        } else {
+          const int u = MODE == 1 ? e : 2 * e, z = MODE == 1 ? 8 + e : 2 * e + 1;
+          if (MODE == 1 || c0 + 2 * e < r.rot) {
+            const f32x2 a = angle(e);
+            const float yu = y[j][u], yz = y[j][z];
+            y[j][u] = fmaf(yu, a.x, -(yz * a.y));
+            y[j][z] = fmaf(yu, a.y, yz * a.x);
+          }
+        }
       }
     }
-    return;
-  }
-  const int half = r.rot >> 1;
-  float o[8];
-  if (half % 8 == 0) {
-    load8(x + (8 * c < half ? 8 * c + half : 8 * c - half), o);
-  } else {
+  };
+  float top = 0.0f;
+  auto look = [&](const float (&y)[kKeep][16]) __attribute__((always_inline)) {   // (repeated last rows do no harm)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int ch = 8 * c + e;
-      o[e] = ch < r.rot ? to_f32(x[ch < half ? ch + half : ch - half]) : 0.0f;
+    for (int j = 0; j < kKeep; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float m = fabsf(y[j][e]);
+        top = m < INFINITY ? fmaxf(top, m) : top;   // false for NaN, too
+      }
+  };
+  const int old = min((int)*g.exponent, 247) - 127;
+  const int batch = kKeep * step;
+  float keep[kKeep][16];
+#pragma unroll 1
+  for (int base = 0; base < g.n; base += batch) {
+    fetch(base, keep);
+    look(keep);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();                               // (also: every thread has read the old exponent)
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) top = fmaxf(top, tops[w]);
+  const int need = need_exp(top), e = g.had > 0 ? max(old, need) : need;
+  if (threadIdx.x == 0) *g.exponent = (uint8_t)(e + 127);
+  const float inv = exp_scale(-e);
+#pragma unroll 1
+  for (int base = 0; base < g.n; base += batch) {
+    if (g.n > batch) fetch(base, keep);
+#pragma unroll
+    for (int j = 0; j < kKeep; ++j) {
+      const int t = base + t0 + j * step;
+      if (t < g.n) {
+        uint8_t* at = g.page + (g.had + t) * g.cs;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float* y = &keep[j][8 * k];
+          *reinterpret_cast<u32x2*>(at + (k == 0 ? c0 : c1)) =
+              u32x2{codes4(y[0], y[1], y[2], y[3], inv), codes4(y[4], y[5], y[6], y[7], inv)};
+        }
+      }
     }
   }
+  // earlier tokens of the page, rounded to the larger exponent
+  if (g.had > 0 && e > old) {
+    const float down = e - old < 127 ? exp_scale(old - e) : 0.0f;
+    for (int t = t0; t < g.had; t += step) {
+      u32x4* at = reinterpret_cast<u32x4*>(g.page + t * g.cs + 16 * item);
+      const u32x4 w = *at;
+      u32x4 o;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int ch = 8 * c + e;
-    if (ch < half) {
-      const f32x2 t = turn(ch);
-      y[e] = fmaf(y[e], t.x, -(o[e] * t.y));
-    } else if (ch < r.rot) {
-      const f32x2 t = turn(ch - half);
-      y[e] = fmaf(o[e], t.y, y[e] * t.x);
+      for (int k = 0; k < 4; ++k) {
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
+        o[k] = codes4(lo.x, lo.y, hi.x, hi.y, down);
+      }
+      *at = o;
     }
   }
 }
 
-// One block per (page of a sequence that the call writes, head, K or V): the largest
-// magnitude of the page's new tokens gives the exponent, then the codes are written.  The
-// call's pages of sequence b are numbered from cu[b] / page + 2 b (a sequence of n tokens
-// meets at most ceil(n / page) + 1 pages, so the ranges do not meet).  Up to kKeep chunks
-// of eight channels a thread stay in registers between the two passes; longer pages are
-// read again (from the L2).
-constexpr int kKeep = 4;
+// One block per (page of a sequence that the call writes, head, K or V).  The call's pages
+// of sequence b are numbered from cu[b] / page + 2 b (a sequence of n tokens meets at most
+// ceil(n / page) + 1 pages, so the ranges do not meet).  KM: how keys are rotated.
+template <int KM>
 __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a) {
   __shared__ f32x2 cs[kTok][kMaxPairs];
   __shared__ int index[kTok], slot[kTok], mine[kTok];
@@ -354,86 +464,18 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a) {
   if (x < div_by(beg, a.s.page) + 2 * b || end <= beg || lo >= hi) return;
   const int id = a.s.table[(long long)b * a.s.max_pages + p];
   if (id < 0 || id >= a.pages) return;
-  const int had = lo - p * a.page;
-  const int row0 = end - (len - lo);             // the call's row of token lo
-  const int cpr = a.dh >> 3, total = (hi - lo) * cpr;
-  const uint16_t* src = is_v ? a.v + h * a.dh : a.k + h * a.dh;
-  const long long ss = is_v ? a.vs : a.ks;
-  uint8_t* page = static_cast<uint8_t*>(is_v ? a.vc : a.kc) + ((long long)id * a.page * a.H + h) * a.dh;
-  uint8_t* ep = (is_v ? a.ve : a.ke) + (long long)id * a.H + h;
-  const long long cs_row = (long long)a.H * a.dh;
-  const int shift = 31 - __clz(cpr);
-  auto get = [&](int i, float* y) {
-    const int t = i >> shift, c = i & (cpr - 1);
-    const uint16_t* xr = src + (long long)(row0 + t) * ss;
-    if (is_v || a.r.rot == 0) load8(xr + 8 * c, y);
-    else rotated8(xr, c, a.r, row0 + t, lo + t, y);
-  };
-  float keep[kKeep][8];
-  float top = 0.0f;
-  auto look = [&](const float* y) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float m = fabsf(y[e]);
-      top = m < INFINITY ? fmaxf(top, m) : top;   // false for NaN, too
-    }
-  };
-#pragma unroll
-  for (int j = 0; j < kKeep; ++j) {
-    const int i = threadIdx.x + j * kThreads;
-    if (i < total) {
-      get(i, keep[j]);
-      look(keep[j]);
-    }
-  }
-  for (int i = threadIdx.x + kKeep * kThreads; i < total; i += kThreads) {
-    float y[8];
-    get(i, y);
-    look(y);
-  }
-  const int old = min((int)*ep, 247) - 127;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-  __syncthreads();                               // (also: every thread has read the old exponent)
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) top = fmaxf(top, tops[w]);
-  const int need = need_exp(top), e = had > 0 ? max(old, need) : need;
-  if (threadIdx.x == 0) *ep = (uint8_t)(e + 127);
-  const float inv = exp_scale(-e);
-  auto put = [&](int i, const float* y) {
-    const int t = i >> shift, c = i & (cpr - 1);
-    uint32_t w[2] = {0u, 0u};
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k >> 2] |= code1(y[k], inv) << (8 * (k & 3));
-    *reinterpret_cast<u32x2*>(page + (had + t) * cs_row + 8 * c) = u32x2{w[0], w[1]};
-  };
-#pragma unroll
-  for (int j = 0; j < kKeep; ++j) {
-    const int i = threadIdx.x + j * kThreads;
-    if (i < total) put(i, keep[j]);
-  }
-  for (int i = threadIdx.x + kKeep * kThreads; i < total; i += kThreads) {
-    float y[8];
-    get(i, y);
-    put(i, y);
-  }
-  // earlier tokens of the page, rounded to the larger exponent
-  if (had > 0 && e > old) {
-    const float down = e - old < 127 ? exp_scale(old - e) : 0.0f;
-    for (int i = threadIdx.x; i < had * cpr; i += kThreads) {
-      u32x2* at = reinterpret_cast<u32x2*>(page + (i >> shift) * cs_row + 8 * (i & (cpr - 1)));
-      const u32x2 w = *at;
-      u32x2 o{0u, 0u};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const f32x2 f = k % 2 == 0 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k >> 1], false)
-                                   : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k >> 1], true);
-        o[k >> 1] |= (code1(f.x, down) | code1(f.y, down) << 8) << (16 * (k & 1));
-      }
-      *at = o;
-    }
-  }
+  PageRows g;
+  g.had = lo - p * a.page;
+  g.n = hi - lo;
+  g.row0 = end - (len - lo);
+  g.index0 = lo;
+  g.ss = is_v ? a.vs : a.ks;
+  g.src = (is_v ? a.v : a.k) + h * a.dh + (long long)g.row0 * g.ss;
+  g.cs = (long long)a.H * a.dh;
+  g.page = static_cast<uint8_t*>(is_v ? a.vc : a.kc) + ((long long)id * a.page * a.H + h) * a.dh;
+  g.exponent = (is_v ? a.ve : a.ke) + (long long)id * a.H + h;
+  if (is_v) store_page<0>(a.r, g, a.dh, tops);
+  else store_page<KM>(a.r, g, a.dh, tops);
 }
 
 // ---------------------------------------------------------------------------
@@ -572,7 +614,11 @@ cast_status_t launch_kv_append(const cast_kv_cache_t& c, const cast_kv_seqs_t& s
     const long long groups = (long long)s.n_tok / c.page + 2ll * s.n_seq;
     const long long blocks = (long long)a.q_blocks_x * a.q_shares + groups * 2 * c.H;
     if (blocks >= (1ll << 31)) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
-    hipLaunchKernelGGL(append8_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+    const dim3 grid((unsigned)blocks);
+    if (a.r.rot == 0) hipLaunchKernelGGL(append8_kernel<0>, grid, dim3(kThreads), 0, stream, a);
+    else if (a.r.inter) hipLaunchKernelGGL(append8_kernel<2>, grid, dim3(kThreads), 0, stream, a);
+    else if (a.r.rot % 16 == 0) hipLaunchKernelGGL(append8_kernel<1>, grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL(append8_kernel<3>, grid, dim3(kThreads), 0, stream, a);
   }
   return check_launch("kv_append");
 }
