@@ -734,7 +734,7 @@ static cast_status_t kv_attn_sizes(const cast_kv_cache_t* cache, const cast_kv_s
 
 static KvAttnPlan make_kv_attn_plan(const cast_kv_cache_t* c, const cast_kv_seqs_t* s, int Hq, int max_len,
                                     int window, int sinks) {
-  return kv_attn_plan(s->n_tok, s->n_seq, Hq / c->H, c->H, c->dh, std::min<long long>(max_len, (long long)s->max_pages * c->page),
+  return kv_attn_plan(s->n_tok, s->n_seq, Hq / c->H, c->H, c->dh, c->dtype == 2, std::min<long long>(max_len, (long long)s->max_pages * c->page),
                       std::min(window, 1 << 30), sinks, device_cu_count());
 }
 

@@ -170,10 +170,11 @@ struct KvAttnPlan {
   int row_tiles;                 // at most, over all ways to share the rows out
   int pieces, piece_tiles;       // 128 rows: pieces along the keys, key tiles of each
   int target, max_items;         // few rows: pieces wanted (0: none is cut), work items at most
+  int wh;                        // few rows: heads of a workgroup
   size_t part_bytes, lse_bytes, bytes;
   bool cut() const { return pieces > 1 || target > 0; }
 };
-KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, long long max_len, int window,
+KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f8, long long max_len, int window,
                         int sinks, int cus);
 cast_status_t launch_kv_attn(const void* q, long long q_stride, int Hq, const cast_kv_cache_t& c,
                              const cast_kv_seqs_t& s, int causal, int window, int sinks, float scale, void* out,

@@ -44,7 +44,12 @@ typedef __attribute__((address_space(3))) char lds_char;
 constexpr int kThreads = 256;
 constexpr int kTileRows = 128;   // rows per workgroup of the tiles kernel
 constexpr int kTileKeys = 64;
-constexpr int kRowKeys = 32;     // keys per tile and wave of the rows kernel
+constexpr int kMinWaveKeys = 128;    // keys that a wave of the rows kernel walks at least, before a range is cut
+// keys per tile and wave of the rows kernel: 16 KB of K and V at 128 channels of bf16, and as
+// much in flight for codes and narrower heads
+constexpr int row_keys(int dh, bool f8) { return dh == 128 && !f8 ? 32 : 64; }
+// its workgroups per compute unit (waves per SIMD)
+constexpr int row_groups(int dh, bool f8, int rows) { return rows == 16 && dh < 128 ? 3 : 2; }
 constexpr int kMaxPieces = 128;
 // s_waitcnt vmcnt(0) that leaves expcnt and lgkmcnt free
 constexpr int kVmcnt0 = 0x0F70;
@@ -64,13 +69,14 @@ struct KvAttnArgs {
   KvSeqs s;
   uint16_t* out;
   float* lse;
-  float* part_o;                 // normalised: [pieces][n_tok * Hq][dh], or [items][rows][dh]
-  float* part_lse;               // log2 domain: [pieces][n_tok * Hq], or [items][rows]
+  float* part_o;                 // normalised: [pieces][n_tok * Hq][dh], or [items][wh][rows][dh]
+  float* part_lse;               // log2 domain: [pieces][n_tok * Hq], or [items][wh][rows]
   int Hq, H, g, pages, page;
   int causal, window, sinks;     // window 0: none
   int npieces, piece_tiles;      // tiles kernel: pieces along the keys, key tiles of each
   int target, max_items;         // rows kernel: pieces wanted (0: none is cut), items at most
-  int2* meta;                    // rows kernel: first item and pieces of [row tile][KV head]
+  int wh, hgroups;               // rows kernel: heads of a workgroup (1, 2 or 4), H / wh
+  int2* meta;                    // rows kernel: first item and pieces of [row tile][head group]
   float sl2;                     // scale * log2(e)
 };
 
@@ -570,24 +576,27 @@ __global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
 // 32x32 tiles need, which leaves room for three workgroups per compute unit, each wave with
 // a whole key tile on its way.  NQ blocks of 16 rows share every key read.
 //
+// The four waves take wh = 4, 2 or 1 neighbouring heads (whatever divides H) and share each
+// head's key tiles 4 / wh ways.  Waves that walk the same tokens in step read them whole
+// lines side by side: with the waves on one head, each 128-byte line of codes was a DRAM
+// access of its own, and 4 contexts of up to 131072 tokens stood at 4.4 TB/s with 33 MB in
+// flight.
+//
 // Work list.  The call's work is shared out by the lengths the device sees, not by their
-// bound: with T the key tiles of all row tiles, a piece is P = max(kMinPiece, T H / target)
-// key tiles, so there are about `target` pieces of like size however ragged the batch.
-// (Cut by the bound on the lengths, 16 streams of 300 to 8100 tokens ran as 2048 workgroups
-// of at most 4 key tiles a wave, half of them empty: 154 us.)  Item x of the list:
-// sequence by sequence, row tile, piece, head (fastest, so that neighbours read
-// neighbouring rows of memory).
-constexpr int kMinPiece = 16;    // key tiles (of 32): four for each wave
-
+// bound: with T the key tiles of all row tiles, a piece is P = T (H / wh) / target key tiles
+// (128 keys a wave at least), so there are about `target` pieces of like size however ragged
+// the batch.  (Cut by the bound on the lengths, 16 streams of 300 to 8100 tokens ran as 2048
+// workgroups of at most 4 key tiles a wave, half of them empty: 154 us.)  Item x of the
+// list: sequence by sequence, row tile, piece, head group (fastest).
 struct Item {
   RowTile t;
-  int h, z, pieces, item0;       // head, piece of `pieces`, item of piece 0 (the next: + H)
+  int hg, z, pieces, item0;      // head group, piece of `pieces`, item of piece 0 (the next: + hgroups)
   int tile_id, per;              // number of the row tile in the call, key tiles of a piece
 };
 struct SeqWork {
   int rt, nt;
 };
-template <int TM>
+template <int TM, int TK>
 __device__ __forceinline__ SeqWork seq_work(const KvAttnArgs& a, int b) {
   SeqWork w{0, 0};
   if (b >= a.s.n_seq) return w;
@@ -595,31 +604,31 @@ __device__ __forceinline__ SeqWork seq_work(const KvAttnArgs& a, int b) {
   if (n <= 0) return w;
   w.rt = (n * a.g + TM - 1) / TM;
   RowTile t;
-  key_tiles<kRowKeys>(a, t, len - n, len - 1, len);
+  key_tiles<TK>(a, t, len - n, len - 1, len);
   w.nt = t.nt;
   return w;
 }
-template <int TM>
+template <int TM, int TK>
 __device__ __forceinline__ bool find_item(const KvAttnArgs& a, int x, Item& it) {
   const int lane = threadIdx.x & 63, n_seq = a.s.n_seq;
-  SeqWork w = seq_work<TM>(a, lane);
+  SeqWork w = seq_work<TM, TK>(a, lane);
   int per = 0x3fffffff;
   if (a.target > 0) {
     float sum = 0.0f;
     for (int c = 0; c < n_seq; c += 64) {
-      const SeqWork v = c == 0 ? w : seq_work<TM>(a, c + lane);
+      const SeqWork v = c == 0 ? w : seq_work<TM, TK>(a, c + lane);
       sum += (float)v.rt * (float)v.nt;
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    // (rounded up, so that the items never pass target + row tiles * H)
-    per = max(kMinPiece, (int)fminf(ceilf(sum * (float)a.H * 1.0001f / (float)a.target), 1.0e9f));
+    // (rounded up, so that the items never pass target + row tiles * hgroups)
+    per = max(kMinWaveKeys / TK * (kThreads / 64 / a.wh), (int)fminf(ceilf(sum * (float)a.hgroups * 1.0001f / (float)a.target), 1.0e9f));
   }
   int base = 0;
   for (int c = 0; c < n_seq; c += 64) {
-    if (c > 0) w = seq_work<TM>(a, c + lane);
+    if (c > 0) w = seq_work<TM, TK>(a, c + lane);
     const int pieces = max(1, (w.nt + per - 1) / per);
-    int incl = w.rt * pieces * a.H;
+    int incl = w.rt * pieces * a.hgroups;
     const int mine = incl;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -632,13 +641,13 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, int x, Item& it) 
       const int first = base + __shfl(incl - mine, l);
       it.pieces = __builtin_amdgcn_readfirstlane(__shfl(pieces, l));
       it.per = per;
-      const int local = __builtin_amdgcn_readfirstlane(x - first), rest = local / a.H;
-      it.h = local - rest * a.H;
+      const int local = __builtin_amdgcn_readfirstlane(x - first), rest = local / a.hgroups;
+      it.hg = local - rest * a.hgroups;
       const int k = rest / it.pieces;
       it.z = rest - k * it.pieces;
-      it.item0 = __builtin_amdgcn_readfirstlane(first) + k * it.pieces * a.H + it.h;
+      it.item0 = __builtin_amdgcn_readfirstlane(first) + k * it.pieces * a.hgroups + it.hg;
       it.tile_id = first_tile<TM>(a, c + l) + k;
-      return place<TM, kRowKeys>(a, c + l, k, it.t);
+      return place<TM, TK>(a, c + l, k, it.t);
     }
     base += __shfl(incl, 63);
   }
@@ -655,8 +664,9 @@ __device__ __forceinline__ float quarter_max(float x) {
 }
 
 template <int DH, bool F8, int NQ>
-__global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAttnArgs a) {
-  constexpr int CPR = DH / 8, ROWB = DH * 2, TK = kRowKeys, W = kThreads / 64, TM = 16 * NQ;
+__global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows_kernel(KvAttnArgs a) {
+  constexpr int CPR = DH / 8, ROWB = DH * 2, TK = row_keys(DH, F8), W = kThreads / 64, TM = 16 * NQ;
+  constexpr int SUB = TK / 32, R = 2 * SUB;          // 32-key halves; a lane's rows: l16 + 16 r
   constexpr int NT = DH / 32;                        // contraction steps of S, 32 channels each
   constexpr int ND = DH / 16;                        // 16-channel blocks of O^T
   // Loads of a lane: rows l16 and l16 + 16 of the tile; bf16 16 bytes (channels 32 i + 8
@@ -664,14 +674,16 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
   // or, of 32-wide heads, 8 bytes for the one step
   constexpr int NL = F8 ? (DH == 32 ? 1 : DH / 64) : NT;
   constexpr bool HALF = F8 && DH == 32;
-  __shared__ __attribute__((aligned(1024))) char smem[W * (TM * DH * 4 > TK * ROWB ? TM * DH * 4 : TK * ROWB)];
+  __shared__ __attribute__((aligned(1024))) char smem[W * (TM * DH * 4 > 32 * ROWB ? TM * DH * 4 : 32 * ROWB)];
   __shared__ float sm[W][TM], sl[W][TM];
 
   Item it;
-  if (!find_item<TM>(a, blockIdx.x, it)) return;
+  if (!find_item<TM, TK>(a, blockIdx.x, it)) return;
   const RowTile& t = it.t;
-  const int h = it.h, tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ways = W / a.wh;                         // waves that share a head's key tiles
+  const int h = it.hg * a.wh + wave % a.wh;
   const int l16 = lane & 15, qd = lane >> 4;
   const int u0 = min(it.z * it.per, t.nt), u1 = min(u0 + min(it.per, t.nt), t.nt);
   const int nrows = min(TM, t.n_rows - t.row0);
@@ -691,11 +703,11 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
   }
   const int32_t* table = a.s.table + (long long)t.b * a.s.max_pages;
   auto tile_of = [&](int u) { return u < t.ts ? u : t.tw + (u - t.ts); };
-  // lanes l and l + 32 look up key l of a tile
+  // lane l looks up key l (mod TK) of a tile
   struct Look { int key, id, rem; };
   auto look = [&](int u) __attribute__((always_inline)) -> Look {
     Look k;
-    k.key = tile_of(min(u, t.nt - 1)) * TK + (lane & 31);
+    k.key = tile_of(min(u, t.nt - 1)) * TK + (lane & (TK - 1));
     const int kk = min(k.key, t.len - 1);
     const int pg = div_by(kk, a.s.page);
     k.id = table[pg];
@@ -704,11 +716,11 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
   };
   const long long row_bytes = (long long)a.H * DH * (F8 ? 1 : 2);
   const int lane_bytes = h * DH * (F8 ? 1 : 2) + qd * (HALF ? 8 : 16);
-  u32x4 kr[2][NL], vr[2][NL];
-  int ke[2], ve[2], ve_cur[2];
-  auto load_rows = [&](const uint8_t* base, const long long (&at)[2], u32x4 (&to)[2][NL]) __attribute__((always_inline)) {
+  u32x4 kr[R][NL], vr[R][NL];
+  int ke[R], ve[R], ve_cur[R];
+  auto load_rows = [&](const uint8_t* base, const long long (&at)[R], u32x4 (&to)[R][NL], int r0, int r1) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
+    for (int r = r0; r < r1; ++r)
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         if constexpr (HALF) {
@@ -719,16 +731,16 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
         }
       }
   };
-  char* vt = smem + wave * (TK * ROWB);
+  char* vt = smem + wave * (32 * ROWB);
   auto vsw = [](int row) { return 2 * ((row / (16 / CPR)) & (CPR / 2 - 1)); };
   // byte offsets in the value tile from which a lane writes and reads; their XORs with a
   // chunk are formed again at each use (opaque() keeps them out of registers across the loop)
   auto opaque = [](unsigned x) { asm volatile("" : "+v"(x)); return x; };
   const unsigned vwr = (unsigned)(l16 * ROWB);
-  auto store_v = [&](unsigned wr) __attribute__((always_inline)) {
+  auto store_v = [&](unsigned wr, int sub) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      char* at = vt + wr + 16 * r * ROWB;      // rows l16 and l16 + 16 have the same swizzle
+    for (int r = 2 * sub; r < 2 * sub + 2; ++r) {
+      char* at = vt + wr + 16 * (r & 1) * ROWB;      // rows l16 and l16 + 16 have the same swizzle
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const u32x4 w = vr[r][i];
@@ -768,14 +780,14 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
   }
 
   unsigned long long there = 0, there_next = 0;
-  long long at[2];
-  // places of the lane's two rows (row 0 of page 0 for keys that do not exist)
+  long long at[R];
+  // places of the lane's rows (row 0 of page 0 for keys that do not exist)
   auto resolve = [&](const Look& k, unsigned long long& th) __attribute__((always_inline)) {
     const bool in = k.id >= 0 && k.id < a.pages;
-    th = __ballot(in && k.key < t.len) & 0xffffffffull;
+    th = __ballot(in && k.key < t.len) & (TK == 64 ? ~0ull : 0xffffffffull);
     const int id = in ? k.id : 0, slot = in ? k.id * a.page + k.rem : 0;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < R; ++r) {
       at[r] = (long long)__shfl(slot, l16 + 16 * r) * row_bytes + lane_bytes;
       if constexpr (F8) {
         const long long pe = (long long)__shfl(id, l16 + 16 * r) * a.H + h;
@@ -785,21 +797,21 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
     }
   };
   Look nxt{};
-  int u = u0 + wave;
+  int u = u0 + wave / a.wh;
   if (u < u1) {
     const Look first = look(u);
     resolve(first, there);
-    load_rows(a.k, at, kr);
-    load_rows(a.v, at, vr);
-    nxt = look(u + W);
+    load_rows(a.k, at, kr, 0, R);
+    load_rows(a.v, at, vr, 0, R);
+    nxt = look(u + ways);
   }
 #pragma unroll 1
-  for (; u < u1; u += W) {
-    const bool more = u + W < u1;
+  for (; u < u1; u += ways) {
+    const bool more = u + ways < u1;
     const int j0 = tile_of(u) * TK;
-    f32x4 sn[NQ][2];
+    f32x4 sn[NQ][R];
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < R; ++r) {
       float sc = 0.0f;
       if constexpr (F8) sc = byte_scale(ke[r]);
 #pragma unroll
@@ -816,51 +828,46 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
       }
     }
     if constexpr (F8) {
-      ve_cur[0] = ve[0];
-      ve_cur[1] = ve[1];
+#pragma unroll
+      for (int r = 0; r < R; ++r) ve_cur[r] = ve[r];
     }
+    const int kind = tile_kind<TK>(a, j0, p0, p1, there);
     if (more) {
       resolve(nxt, there_next);
-      load_rows(a.k, at, kr);
-      nxt = look(u + 2 * W);
+      load_rows(a.k, at, kr, 0, R);
+      nxt = look(u + 2 * ways);
     }
-    store_v(opaque(vwr));
-    const unsigned vrd = opaque(vrd0);
-    const int kind = tile_kind<TK>(a, j0, p0, p1, there);
-    bool special = false;
-    if (kind == 1) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int db = 0; db < ND; ++db) m |= special_bits(read_v(vrd, db));
-      special = __ballot((m & 0x80008000u) != 0) != 0ull;
-    }
-    // (special tiles fetch the next values later: together with them they need more registers)
-    if (more && !special) load_rows(a.v, at, vr);
+    bf16x8 pp[NQ][SUB];
     if (kind != 0) {
       if (kind == 1) {
 #pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) {
-          const uint32_t bits = visible_bits(lim[nq], a.sinks, j0, (uint32_t)there) >> (4 * qd);
+        for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (((bits >> (16 * (e / 4) + e % 4)) & 1) == 0) sn[nq][e / 4][e % 4] = -INFINITY;
-        }
+          for (int sub = 0; sub < SUB; ++sub) {
+            const uint32_t bits = visible_bits(lim[nq], a.sinks, j0 + 32 * sub, (uint32_t)(there >> (32 * sub))) >> (4 * qd);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (((bits >> (16 * (e / 4) + e % 4)) & 1) == 0) sn[nq][2 * sub + e / 4][e % 4] = -INFINITY;
+          }
       }
-      bf16x8 pp[NQ];
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) {
         // (see softmax)
-        float pe[8];
+        float pe[8 * SUB];
         auto exps = [&]() __attribute__((always_inline)) -> float {
+          float rs[4];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) pe[e] = __builtin_amdgcn_exp2f(fmaf(sn[nq][e / 4][e % 4], a.sl2, -m_run[nq]));
-          return ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
+          for (int e = 0; e < 8 * SUB; ++e) {
+            pe[e] = __builtin_amdgcn_exp2f(fmaf(sn[nq][e / 4][e % 4], a.sl2, -m_run[nq]));
+            rs[e % 4] = e < 4 ? pe[e] : rs[e % 4] + pe[e];
+          }
+          return (rs[0] + rs[1]) + (rs[2] + rs[3]);
         };
         float sum = exps();
         if (__ballot(!(sum <= 256.0f)) != 0ull) {
           float pm = sn[nq][0][0];
 #pragma unroll
-          for (int e = 1; e < 8; ++e) pm = fmaxf(pm, sn[nq][e / 4][e % 4]);
+          for (int e = 1; e < 8 * SUB; ++e) pm = fmaxf(pm, sn[nq][e / 4][e % 4]);
           const float cand = fmaxf(m_run[nq], quarter_max(pm) * a.sl2);
           const bool up = cand > m_run[nq] + kMaxSlack;
           const float m_new = up ? cand : m_run[nq];
@@ -871,16 +878,36 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
           for (int db = 0; db < ND; ++db) acc[nq][db] *= corr;
           sum = exps();
         }
-        pp[nq] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(pe[0], pe[1]), pack_bf16x2(pe[2], pe[3]),
-                                                  pack_bf16x2(pe[4], pe[5]), pack_bf16x2(pe[6], pe[7])});
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub) {
+          const float* p = &pe[8 * sub];
+          pp[nq][sub] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
+                                                         pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])});
+        }
         l_run[nq] += sum;
       }
+    }
+    // values, 32 keys at a time through the wave's LDS tile
+#pragma unroll
+    for (int sub = 0; sub < SUB; ++sub) {
+      store_v(opaque(vwr), sub);
+      const unsigned vrd = opaque(vrd0);
+      bool special = false;
+      if (kind == 1) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int db = 0; db < ND; ++db) m |= special_bits(read_v(vrd, db));
+        special = __ballot((m & 0x80008000u) != 0) != 0ull;
+      }
+      // (special tiles fetch the next values later: together with them they need more registers)
+      if (more && !special) load_rows(a.v, at, vr, 2 * sub, 2 * sub + 2);
+      if (kind == 0) continue;
       if (!special) {
 #pragma unroll
         for (int db = 0; db < ND; ++db) {
           const bf16x8 op = read_v(vrd, db);
 #pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) acc[nq][db] = mfma16(op, pp[nq], acc[nq][db]);
+          for (int nq = 0; nq < NQ; ++nq) acc[nq][db] = mfma16(op, pp[nq][sub], acc[nq][db]);
         }
       } else {
 #pragma unroll
@@ -889,18 +916,18 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
 #pragma unroll
           for (int nq = 0; nq < NQ; ++nq) {
             const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
-            const bf16x8 w = seen_weights(pp[nq]);
-            acc[nq][db] = mfma16(v.fin, pp[nq], acc[nq][db]);
+            const bf16x8 w = seen_weights(pp[nq][sub]);
+            acc[nq][db] = mfma16(v.fin, pp[nq][sub], acc[nq][db]);
             add_special<4>(acc[nq][db], mfma16(v.pos, w, zero), mfma16(v.neg, w, zero));
           }
         }
-        if (more) load_rows(a.v, at, vr);
+        if (more) load_rows(a.v, at, vr, 2 * sub, 2 * sub + 2);
       }
     }
     there = there_next;
   }
 
-  // ---- join the four waves: weights 2^(m_w - max m)
+  // ---- join the waves of a head: weights 2^(m_w - max m)
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
     float l = l_run[nq] + __shfl_xor(l_run[nq], 16);
@@ -910,7 +937,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
       sl[wave][16 * nq + l16] = l;
     }
   }
-  __syncthreads();
+  __syncthreads();                                   // (the value tiles are read no more)
   float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq)
@@ -920,75 +947,98 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void kv_rows_kernel(KvAt
         *reinterpret_cast<f32x4*>(part + (wave * TM + 16 * nq + l16) * DH + 16 * db + 4 * qd) = acc[nq][db];
     }
   __syncthreads();
-  const long long item = blockIdx.x;
-  if (a.target > 0 && it.z == 0 && tid == 0) a.meta[(long long)it.tile_id * a.H + h] = make_int2(it.item0, it.pieces);
-  for (int i = tid; i < nrows * (DH / 4); i += kThreads) {
-    const int ql = i / (DH / 4), d = 4 * (i % (DH / 4));
-    float m = sm[0][ql];
-#pragma unroll
-    for (int w = 1; w < W; ++w) m = fmaxf(m, sm[w][ql]);
+  if (a.target > 0 && it.z == 0 && tid == 0) a.meta[(long long)it.tile_id * a.hgroups + it.hg] = make_int2(it.item0, it.pieces);
+  const int per_head = nrows * (DH / 4);
+  for (int i = tid; i < a.wh * per_head; i += kThreads) {
+    const int hw = i / per_head, j = i - hw * per_head;
+    const int ql = j / (DH / 4), d = 4 * (j % (DH / 4));
+    float m = kNoMax;
+    for (int w = hw; w < W; w += a.wh) m = fmaxf(m, sm[w][ql]);
     float lt = 0.0f;
     f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      if (sl[w][ql] == 0.0f) continue;         // saw no key
+    for (int w = hw; w < W; w += a.wh) {
+      if (sl[w][ql] == 0.0f) continue;               // saw no key
       const float c = __builtin_amdgcn_exp2f(sm[w][ql] - m);
       lt += c * sl[w][ql];
       o += c * *reinterpret_cast<const f32x4*>(part + (w * TM + ql) * DH + d);
     }
-    const bool some = lt != 0.0f;              // true for NaN, too
+    const bool some = lt != 0.0f;                    // true for NaN, too
     o *= some ? 1.0f / lt : 0.0f;
     const float l2 = some ? m + __log2f(lt) : -INFINITY;
     if (it.pieces > 1) {
-      *reinterpret_cast<f32x4*>(a.part_o + (item * TM + ql) * DH + d) = o;
-      if (d == 0) a.part_lse[item * TM + ql] = l2;
+      const long long at = ((long long)blockIdx.x * a.wh + hw) * TM + ql;
+      *reinterpret_cast<f32x4*>(a.part_o + at * DH + d) = o;
+      if (d == 0) a.part_lse[at] = l2;
     } else {
       const int rr = t.row0 + ql, tk = rr / a.g;
-      const long long row = (long long)(t.beg + tk) * a.Hq + h * a.g + (rr - tk * a.g);
+      const long long row = (long long)(t.beg + tk) * a.Hq + (it.hg * a.wh + hw) * a.g + (rr - tk * a.g);
       put4(a, row, DH, d, o);
       if (a.lse != nullptr && d == 0) a.lse[row] = l2 * kLn2;
     }
   }
 }
 
-// Join of the pieces of a row tile that the rows kernel cut: with l_z the log2 log-sum-exp
-// and O_z the normalised output of piece z, O = sum 2^(l_z - max) O_z / sum 2^(l_z - max).
-// Pieces without a visible key (-inf) add nothing.
+// Join of the pieces of a row that the rows kernel cut: with l_z the log2 log-sum-exp and
+// O_z the normalised output of piece z, O = sum 2^(l_z - max) O_z / sum 2^(l_z - max).
+// Pieces without a visible key (-inf) add nothing.  One workgroup per row, its threads
+// shared out over four channels each and, in step, the pieces; grid (row tile, head, row).
 template <int DH, int TM>
 __global__ __launch_bounds__(kThreads) void kv_rows_join_kernel(KvAttnArgs a) {
+  constexpr int PER = DH / 4, WAYS = kThreads / PER;
+  __shared__ float red[kThreads / 64];
+  __shared__ f32x4 part[kThreads];
+  __shared__ float sums[WAYS];
   RowTile t;
-  if (!row_tile<TM, kRowKeys>(a, blockIdx.x, t)) return;
-  const int2 meta = a.meta[(long long)blockIdx.x * a.H + blockIdx.y];
+  if (!row_tile<TM, 32>(a, blockIdx.x, t)) return;
+  const int ql = blockIdx.z, tid = threadIdx.x;
+  if (ql >= t.n_rows - t.row0) return;
+  const int hg = blockIdx.y / a.wh, hw = blockIdx.y - hg * a.wh;
+  const int2 meta = a.meta[(long long)blockIdx.x * a.hgroups + hg];
   // (the bounds hold for whatever lies in the workspace)
-  if (meta.y < 2 || meta.x < 0 || meta.x >= a.max_items || meta.y > (a.max_items - 1 - meta.x) / a.H + 1) return;
-  const int nrows = min(TM, t.n_rows - t.row0);
-  for (int i = threadIdx.x; i < nrows * (DH / 4); i += kThreads) {
-    const int ql = i / (DH / 4), d = 4 * (i % (DH / 4));
-    auto lse_of = [&](int z) { return a.part_lse[(long long)(meta.x + z * a.H) * TM + ql]; };
-    float m = -INFINITY;
-    for (int z = 0; z < meta.y; ++z) {
-      const float l = lse_of(z);
-      m = l > m || l != l ? l : m;
-    }
-    float w = 0.0f;
-    f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int z = 0; z < meta.y; ++z) {
-      const float l = lse_of(z);
-      const f32x4 p = *reinterpret_cast<const f32x4*>(a.part_o + ((long long)(meta.x + z * a.H) * TM + ql) * DH + d);
-      const float c = l == m ? 1.0f : __builtin_amdgcn_exp2f(l - m);
-      if (l != -INFINITY) {
-        w += c;
-        o += c * p;
-      }
-    }
-    const bool some = w != 0.0f;
-    o *= some ? 1.0f / w : 0.0f;
-    const int rr = t.row0 + ql, tk = rr / a.g;
-    const long long row = (long long)(t.beg + tk) * a.Hq + blockIdx.y * a.g + (rr - tk * a.g);
-    put4(a, row, DH, d, o);
-    if (a.lse != nullptr && d == 0) a.lse[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
+  if (meta.y < 2 || meta.x < 0 || meta.x >= a.max_items || meta.y > (a.max_items - 1 - meta.x) / a.hgroups + 1) return;
+  auto slot = [&](int z) { return ((long long)(meta.x + z * a.hgroups) * a.wh + hw) * TM + ql; };
+  float m = -INFINITY;
+  for (int z = tid; z < meta.y; z += kThreads) {
+    const float l = a.part_lse[slot(z)];
+    m = l > m || l != l ? l : m;
   }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const float o = __shfl_xor(m, d);
+    m = o > m || o != o ? o : m;
+  }
+  if ((tid & 63) == 0) red[tid >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) m = red[w] > m || red[w] != red[w] ? red[w] : m;
+  const int way = tid / PER, d = 4 * (tid % PER);
+  float w = 0.0f;
+  f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int z = way; z < meta.y; z += WAYS) {
+    const float l = a.part_lse[slot(z)];
+    const f32x4 p = *reinterpret_cast<const f32x4*>(a.part_o + slot(z) * DH + d);
+    const float c = l == m ? 1.0f : __builtin_amdgcn_exp2f(l - m);
+    if (l != -INFINITY) {
+      w += c;
+      o += c * p;
+    }
+  }
+  part[tid] = o;
+  if (d == 0) sums[way] = w;
+  __syncthreads();
+  if (way != 0) return;
+#pragma unroll 1
+  for (int k = 1; k < WAYS; ++k) {
+    w += sums[k];
+    o += part[k * PER + tid];
+  }
+  const bool some = w != 0.0f;
+  o *= some ? 1.0f / w : 0.0f;
+  const int rr = t.row0 + ql, tk = rr / a.g;
+  const long long row = (long long)(t.beg + tk) * a.Hq + blockIdx.y * a.g + (rr - tk * a.g);
+  put4(a, row, DH, d, o);
+  if (a.lse != nullptr && d == 0) a.lse[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
 }
 
 // Join of the pieces of every row: with l_z the log2 log-sum-exp and O_z the normalised
@@ -1025,10 +1075,10 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(KvAttnArgs a) {
 
 template <int DH, bool F8, int NQ>
 void launch_rows(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
-  const int items = p.target > 0 ? p.max_items : p.row_tiles * a.H;
+  const int items = p.target > 0 ? p.max_items : p.row_tiles * a.hgroups;
   hipLaunchKernelGGL((kv_rows_kernel<DH, F8, NQ>), dim3(items), dim3(kThreads), 0, stream, a);
   if (p.target > 0)
-    hipLaunchKernelGGL((kv_rows_join_kernel<DH, 16 * NQ>), dim3(p.row_tiles, a.H), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((kv_rows_join_kernel<DH, 16 * NQ>), dim3(p.row_tiles, a.H, 16 * NQ), dim3(kThreads), 0, stream, a);
 }
 
 template <int DH, bool F8>
@@ -1045,31 +1095,31 @@ void launch_as(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
 
 }  // namespace
 
-KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, long long max_len, int window, int sinks,
+KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f8, long long max_len, int window, int sinks,
                         int cus) {
   KvAttnPlan p{};
   const long long rows = n_tok * g, mean = (rows + n_seq - 1) / n_seq;
   p.rows = mean <= 16 ? 16 : mean <= 64 ? 32 : kTileRows;
-  const int tk = p.rows == kTileRows ? kTileKeys : kRowKeys;
+  p.wh = H % 4 == 0 ? 4 : H % 2 == 0 ? 2 : 1;
   p.row_tiles = (int)(rows / p.rows + n_seq);
   p.pieces = 1;
   p.piece_tiles = 1;
   if (cus <= 0 || n_tok < 1) return p;
-  const long long units = (long long)n_seq * ((mean + p.rows - 1) / p.rows) * H;
+  const long long tiles = (long long)n_seq * ((mean + p.rows - 1) / p.rows);
   long long keys = max_len;
-  if (window > 0) keys = std::min(keys, (long long)window + (mean + g - 1) / g + sinks + 2 * tk);
-  const long long nt = (keys + tk - 1) / tk;
+  if (window > 0) keys = std::min(keys, (long long)window + (mean + g - 1) / g + sinks + 2 * kTileKeys);
   if (p.rows < kTileRows) {
     // workgroups resident at once, less the partial pieces that the row tiles end with
-    const long long resident = (long long)cus * (p.rows == 16 ? 3 : 2);
-    if (nt <= kMinPiece || units >= resident) return p;
+    const long long resident = (long long)cus * row_groups(dh, f8, p.rows), units = tiles * (H / p.wh);
+    if (keys <= kMinWaveKeys * (kThreads / 64 / p.wh) || units >= resident) return p;
     p.target = (int)std::max(resident - units / 2, resident / 2);
-    p.max_items = p.target + p.row_tiles * H + 1;
-    p.part_bytes = align_up((size_t)p.max_items * p.rows * dh * 4);
-    p.lse_bytes = align_up((size_t)p.max_items * p.rows * 4);
-    p.bytes = p.part_bytes + p.lse_bytes + align_up((size_t)p.row_tiles * H * sizeof(int2));
+    p.max_items = p.target + p.row_tiles * (H / p.wh) + 1;
+    p.part_bytes = align_up((size_t)p.max_items * p.wh * p.rows * dh * 4);
+    p.lse_bytes = align_up((size_t)p.max_items * p.wh * p.rows * 4);
+    p.bytes = p.part_bytes + p.lse_bytes + align_up((size_t)p.row_tiles * (H / p.wh) * sizeof(int2));
     return p;
   }
+  const long long units = tiles * H, nt = (keys + kTileKeys - 1) / kTileKeys;
   const long long want = (long long)cus * 2 / std::max(units, 1ll);
   const long long most = std::min<long long>(std::min<long long>(want, kMaxPieces), (nt + 7) / 8);   // 8 key tiles at least
   if (most < 2) return p;
@@ -1097,6 +1147,8 @@ cast_status_t launch_kv_attn(const void* q, long long q_stride, int Hq, const ca
   a.part_o = static_cast<float*>(workspace);
   a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.part_bytes);
   a.meta = reinterpret_cast<int2*>(static_cast<char*>(workspace) + plan.part_bytes + plan.lse_bytes);
+  a.wh = plan.wh;
+  a.hgroups = c.H / plan.wh;
   a.target = plan.target;
   a.max_items = plan.max_items;
   a.Hq = Hq;
