@@ -74,6 +74,7 @@ struct KvAttnArgs {
   int Hq, H, g, pages, page;
   int causal, window, sinks;     // window 0: none
   int npieces, piece_tiles;      // tiles kernel: pieces along the keys, key tiles of each
+  int row_tiles;
   int target, max_items;         // rows kernel: pieces wanted (0: none is cut), items at most
   int wh, hgroups;               // rows kernel: heads of a workgroup (1, 2 or 4), H / wh
   int2* meta;                    // rows kernel: first item and pieces of [row tile][head group]
@@ -365,13 +366,24 @@ __global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) uint16_t lds_v0[TK * DH];
   __shared__ __attribute__((aligned(1024))) uint16_t lds_v1[TK * DH];
 
+  // Workgroup b runs on XCD b mod 8.  Each XCD takes a run of the (head, piece, row tile)
+  // list, so the row tiles that read the same keys share its L2, and walks it from the end:
+  // of causal rows the last tiles are the longest, and the shortest should finish the call.
+  int z, h;
   RowTile t;
-  if (!row_tile<kTileRows, TK>(a, blockIdx.x, t)) return;
-  const int h = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  {
+    const int n = gridDim.x, b = blockIdx.x, x = b & 7, j = b >> 3, per = n >> 3, rest = n & 7;
+    const int unit = x * per + min(x, rest) + (per + (x < rest ? 1 : 0)) - 1 - j;
+    const int q = unit / a.row_tiles;
+    h = q / a.npieces;
+    z = q - h * a.npieces;
+    if (!row_tile<kTileRows, TK>(a, unit - q * a.row_tiles, t)) return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hf = lane >> 5;
   int u0, u1;
-  piece_range(a, t.nt, blockIdx.z, u0, u1);
+  piece_range(a, t.nt, z, u0, u1);
 
   // the lane's row; rows past the end repeat the last one and are not stored
   const int w0 = t.row0 + wave * 32;
@@ -548,7 +560,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
   const float l2 = l > 0.0f || l != l ? m_run + __log2f(l) : -INFINITY;
   const long long row = (long long)(t.beg + tok) * a.Hq + hq;
   if (a.npieces > 1) {
-    const long long at = (long long)blockIdx.z * a.s.n_tok * a.Hq + row;
+    const long long at = (long long)z * a.s.n_tok * a.Hq + row;
     if (hf == 0) a.part_lse[at] = l2;
     if (u0 < u1) {
 #pragma unroll
@@ -1085,7 +1097,7 @@ template <int DH, bool F8>
 void launch_as(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
   if (p.rows == 16) return launch_rows<DH, F8, 1>(a, p, stream);
   if (p.rows == 32) return launch_rows<DH, F8, 2>(a, p, stream);
-  hipLaunchKernelGGL((kv_tiles_kernel<DH, F8>), dim3(p.row_tiles, a.H, p.pieces), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((kv_tiles_kernel<DH, F8>), dim3(p.row_tiles * a.H * p.pieces), dim3(kThreads), 0, stream, a);
   if (p.pieces > 1) {
     const long long threads = (long long)a.s.n_tok * a.Hq * (DH / 4);
     hipLaunchKernelGGL((kv_join_kernel<DH>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
@@ -1160,6 +1172,7 @@ cast_status_t launch_kv_attn(const void* q, long long q_stride, int Hq, const ca
   a.window = window;
   a.sinks = window > 0 ? sinks : 0;
   a.npieces = plan.pieces;
+  a.row_tiles = plan.row_tiles;
   a.piece_tiles = plan.piece_tiles;
   a.sl2 = scale * 1.4426950408889634f;
   const bool f8 = c.dtype == 2;
