@@ -168,6 +168,21 @@ __device__ __forceinline__ void piece_range(const KvAttnArgs& a, int nt, int z, 
   u1 = min(u0 + per, nt);
 }
 
+// The head, piece and row tile of a workgroup of the tiles kernels.  Workgroup b runs on
+// XCD b mod 8.  Each XCD takes a run of the (head, piece, row tile) list, so the row tiles
+// that read the same keys share its L2, and walks it from the end: of causal rows the last
+// tiles are the longest, and the shortest should finish the call.  (With heads over all XCDs
+// and short tiles first: prompts 463 us for 425, chunks of 64-wide heads 232 for 195.)
+template <int TM, int TK>
+__device__ __forceinline__ bool my_unit(const KvAttnArgs& a, int& z, int& h, RowTile& t) {
+  const int n = gridDim.x, b = blockIdx.x, x = b & 7, j = b >> 3, per = n >> 3, rest = n & 7;
+  const int unit = x * per + min(x, rest) + (per + (x < rest ? 1 : 0)) - 1 - j;
+  const int q = unit / a.row_tiles;
+  h = q / a.npieces;
+  z = q - h * a.npieces;
+  return row_tile<TM, TK>(a, unit - q * a.row_tiles, t);
+}
+
 // A lane's row, and which keys it sees: j < hi, and j >= lo or j < sinks.
 struct RowLimits {
   int hi, lo;
@@ -210,24 +225,28 @@ __device__ __forceinline__ void mask_scores(f32x16 (&sn)[NB], int j0, int hf, Ro
   }
 }
 
-// Exponentials of a tile against the running maximum, packed as P^T operands, and their
-// sum.  A lane's sum of at most 2^8 shows that no score is far above the maximum, which
-// then may stay (probabilities up to 2^8 do no harm in fp32 sums and bf16 operands); else
-// the maximum is taken over the tile, moved, and the sums so far scaled down.
-template <int NB, int ND>
-__device__ __forceinline__ void softmax(const f32x16 (&sn)[NB], bf16x8 (&pp)[NB][2], float& m_run, float& l_run,
+// Exponentials of a tile against the running maximum, in place of the scores (a second set
+// would cost the registers of two waves per SIMD at 64-wide heads), packed as P^T operands,
+// and their sum.  A lane's sum of at most 2^8 shows that no score is far above the maximum,
+// which then may stay (probabilities up to 2^8 do no harm in fp32 sums and bf16 operands);
+// else the scores are formed again, the maximum is taken over the tile, moved, and the sums
+// so far scaled down.
+template <int NB, int ND, class S>
+__device__ __forceinline__ void softmax(f32x16 (&sn)[NB], S&& scores, bf16x8 (&pp)[NB][2], float& m_run, float& l_run,
                                         f32x16 (&acc)[ND], float sl2) {
-  float pe[NB * 16], rs[4];
   auto exps = [&]() __attribute__((always_inline)) -> float {
+    float rs[4];
 #pragma unroll
     for (int e = 0; e < NB * 16; ++e) {
-      pe[e] = __builtin_amdgcn_exp2f(fmaf(sn[e / 16][e % 16], sl2, -m_run));
-      rs[e % 4] = e < 4 ? pe[e] : rs[e % 4] + pe[e];
+      const float p = __builtin_amdgcn_exp2f(fmaf(sn[e / 16][e % 16], sl2, -m_run));
+      sn[e / 16][e % 16] = p;
+      rs[e % 4] = e < 4 ? p : rs[e % 4] + p;
     }
     return (rs[0] + rs[1]) + (rs[2] + rs[3]);
   };
   float sum = exps();
   if (__ballot(!(sum <= 256.0f)) != 0ull) {
+    scores();
     float pm = sn[0][0];
 #pragma unroll
     for (int e = 1; e < NB * 16; ++e) pm = fmaxf(pm, sn[e / 16][e % 16]);
@@ -245,9 +264,10 @@ __device__ __forceinline__ void softmax(const f32x16 (&sn)[NB], bf16x8 (&pp)[NB]
   }
 #pragma unroll
   for (int g = 0; g < 2 * NB; ++g) {
-    const float* p = &pe[8 * g];
-    pp[g / 2][g % 2] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
-                                                        pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])});
+    const f32x16& p = sn[g / 2];
+    const int b = 8 * (g % 2);
+    pp[g / 2][g % 2] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[b], p[b + 1]), pack_bf16x2(p[b + 2], p[b + 3]),
+                                                        pack_bf16x2(p[b + 4], p[b + 5]), pack_bf16x2(p[b + 6], p[b + 7])});
   }
   l_run += sum;
 }
@@ -271,6 +291,7 @@ __device__ __forceinline__ void values(R&& read, const bf16x8 (&pp)[NB][2], f32x
     constexpr int u = decltype(uu)::value;
     if constexpr (u + AHEAD < N) rd(IC<u + AHEAD>{});
     acc[u % ND] = mfma(op[u], pp[u / (2 * ND)][(u / ND) % 2], acc[u % ND]);
+    __builtin_amdgcn_sched_barrier(0);
   });
 }
 
@@ -284,21 +305,18 @@ __device__ __forceinline__ uint32_t special_bits(bf16x8 op) {
   const u32x4 w = __builtin_bit_cast(u32x4, op);
   return (special_bits(w.x) | special_bits(w.y)) | (special_bits(w.z) | special_bits(w.w));
 }
-struct Images {
-  bf16x8 fin, pos, neg;
-};
-__device__ __forceinline__ Images images(bf16x8 op) {
-  const u32x4 w = __builtin_bit_cast(u32x4, op);
-  u32x4 f, p, n;
+enum Part { kFinite, kPlus, kMinus };
+template <Part P>
+__device__ __forceinline__ bf16x8 part_of(bf16x8 op) {
+  u32x4 w = __builtin_bit_cast(u32x4, op);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t m = special_bits(w[i]) & 0x80008000u;
     const uint32_t nan = m & (((w[i] & 0x007f007fu) + 0x007f007fu) << 8), sign = w[i] & 0x80008000u;
-    f[i] = w[i] & ~((m >> 15) * 0xffffu);
-    p[i] = ((m & (~sign | nan)) >> 15) * 0x3f80u;
-    n[i] = ((m & (sign | nan)) >> 15) * 0x3f80u;
+    if (P == kFinite) w[i] &= ~((m >> 15) * 0xffffu);
+    else w[i] = ((m & ((P == kPlus ? ~sign : sign) | nan)) >> 15) * 0x3f80u;
   }
-  return Images{__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, p), __builtin_bit_cast(bf16x8, n)};
+  return __builtin_bit_cast(bf16x8, w);
 }
 // 1 where a weight is not zero
 __device__ __forceinline__ bf16x8 seen_weights(bf16x8 p8) {
@@ -307,41 +325,57 @@ __device__ __forceinline__ bf16x8 seen_weights(bf16x8 p8) {
   for (int i = 0; i < 4; ++i) p[i] = ((((p[i] & 0x7fff7fffu) + 0x7fff7fffu) & 0x80008000u) >> 15) * 0x3f80u;
   return __builtin_bit_cast(bf16x8, p);
 }
-// pos, neg: counts; one above 0 times 3e38 twice is infinite (not fused with the sums, which
-// would take the product without its overflow)
+// Adds infinity times the sign where the count is above 0: the count times 3e38 twice (not
+// fused with the sum, which would take the product without its overflow).
 template <int N, class V>
-__device__ __forceinline__ void add_special(V& acc, V pos, V neg) {
+__device__ __forceinline__ void add_infinity(V& acc, V count, float sign) {
 #pragma clang fp contract(off)
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-    const float p = pos[e] * 3.0e38f, n = neg[e] * 3.0e38f;
-    acc[e] += p * 3.0e38f - n * 3.0e38f;
+    const float c = count[e] * 3.0e38f;
+    acc[e] += c * (3.0e38f * sign);
   }
-  asm volatile("" : "+v"(acc));   // done before the next block of channels begins: fewer registers
 }
+// A step of the special products is done before the next begins: they are rare and should
+// not cost the loop around them registers.
+#define PIN(x) asm volatile("" : "+v"(x))
 template <int NB, int ND, class R>
 __device__ __forceinline__ bool has_special(R&& read) {
   uint32_t m = 0;
 #pragma unroll
   for (int g = 0; g < 2 * NB; ++g)
 #pragma unroll
-    for (int db = 0; db < ND; ++db) m |= special_bits(read(db, g / 2, g % 2));
+    for (int db = 0; db < ND; ++db) {
+      m |= special_bits(read(db, g / 2, g % 2));
+      PIN(m);
+    }
   return __ballot((m & 0x80008000u) != 0) != 0ull;
 }
 template <int NB, int ND, class R>
 __device__ __forceinline__ void values_special(R&& read, const bf16x8 (&pp)[NB][2], f32x16 (&acc)[ND]) {
 #pragma unroll
   for (int db = 0; db < ND; ++db) {
-    f32x16 pos{}, neg{};
 #pragma unroll
     for (int g = 0; g < 2 * NB; ++g) {
-      const Images v = images(read(db, g / 2, g % 2));
-      const bf16x8 w = seen_weights(pp[g / 2][g % 2]);
-      acc[db] = mfma(v.fin, pp[g / 2][g % 2], acc[db]);
-      pos = mfma(v.pos, w, pos);
-      neg = mfma(v.neg, w, neg);
+      acc[db] = mfma(part_of<kFinite>(read(db, g / 2, g % 2)), pp[g / 2][g % 2], acc[db]);
+      PIN(acc[db]);
     }
-    add_special<16>(acc[db], pos, neg);
+    f32x16 count{};
+#pragma unroll
+    for (int g = 0; g < 2 * NB; ++g) {
+      count = mfma(part_of<kPlus>(read(db, g / 2, g % 2)), seen_weights(pp[g / 2][g % 2]), count);
+      PIN(count);
+    }
+    add_infinity<16>(acc[db], count, 1.0f);
+    PIN(acc[db]);
+    count = f32x16{};
+#pragma unroll
+    for (int g = 0; g < 2 * NB; ++g) {
+      count = mfma(part_of<kMinus>(read(db, g / 2, g % 2)), seen_weights(pp[g / 2][g % 2]), count);
+      PIN(count);
+    }
+    add_infinity<16>(acc[db], count, -1.0f);
+    PIN(acc[db]);
   }
 }
 
@@ -350,11 +384,37 @@ __device__ __forceinline__ void put4(const KvAttnArgs& a, long long row, int dh,
   *reinterpret_cast<u32x2*>(a.out + row * dh + d) = u32x2{pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w)};
 }
 
+// A lane's row of a tiles kernel: normalised into the output, or as piece z of it.
+template <int DH, int ND>
+__device__ __forceinline__ void finish(const KvAttnArgs& a, int z, long long row, int hf, bool any, float m_run,
+                                       float l_run, const f32x16 (&acc)[ND]) {
+  const float l = l_run + __shfl_xor(l_run, 32);
+  const bool some = l != 0.0f;               // true for NaN, too
+  const float inv = some ? 1.0f / l : 0.0f;
+  const float l2 = some ? m_run + __log2f(l) : -INFINITY;
+  const long long at = (long long)z * a.s.n_tok * a.Hq + row;
+  if (a.npieces > 1) {
+    if (hf == 0) a.part_lse[at] = l2;
+    if (!any) return;
+  } else if (a.lse != nullptr && hf == 0) {
+    a.lse[row] = l2 * kLn2;
+  }
+#pragma unroll
+  for (int db = 0; db < ND; ++db)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+      const f32x4 o{acc[db][4 * g4] * inv, acc[db][4 * g4 + 1] * inv, acc[db][4 * g4 + 2] * inv, acc[db][4 * g4 + 3] * inv};
+      const int d = db * 32 + 8 * g4 + 4 * hf;
+      if (a.npieces > 1) *reinterpret_cast<f32x4*>(a.part_o + at * DH + d) = o;
+      else put4(a, row, DH, d, o);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // tiles
 // ---------------------------------------------------------------------------
 template <int DH, bool F8>
-__global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv_tiles_kernel(KvAttnArgs a) {
   constexpr int CPR = DH / 8, ROWB = DH * 2, ND = DH / 32, TK = kTileKeys;
   constexpr int NSLOT = DH / 32;             // 1-KB copies of a bf16 tile per wave
   constexpr int RSTEP = 2048 / DH;           // tile rows between them
@@ -366,19 +426,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) uint16_t lds_v0[TK * DH];
   __shared__ __attribute__((aligned(1024))) uint16_t lds_v1[TK * DH];
 
-  // Workgroup b runs on XCD b mod 8.  Each XCD takes a run of the (head, piece, row tile)
-  // list, so the row tiles that read the same keys share its L2, and walks it from the end:
-  // of causal rows the last tiles are the longest, and the shortest should finish the call.
   int z, h;
   RowTile t;
-  {
-    const int n = gridDim.x, b = blockIdx.x, x = b & 7, j = b >> 3, per = n >> 3, rest = n & 7;
-    const int unit = x * per + min(x, rest) + (per + (x < rest ? 1 : 0)) - 1 - j;
-    const int q = unit / a.row_tiles;
-    h = q / a.npieces;
-    z = q - h * a.npieces;
-    if (!row_tile<kTileRows, TK>(a, unit - q * a.row_tiles, t)) return;
-  }
+  if (!my_unit<kTileRows, TK>(a, z, h, t)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hf = lane >> 5;
@@ -524,18 +574,23 @@ __global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
     const int kind = live ? tile_kind<TK>(a, j0, p0, p1, there) : 0;
     if (kind != 0) {
       f32x16 sn[2];
-      constexpr int N = 2 * (DH / 16), AHEAD = 3;
-      const unsigned kb0 = opaque(kbase), vb0 = opaque(vbase);
-      bf16x8 op[N];
-      static_for<0, AHEAD>([&](auto uu) { constexpr int i = decltype(uu)::value; op[i] = read_k(kt, kb0, i / 2, i % 2); });
-      static_for<0, N>([&](auto uu) {
-        constexpr int i = decltype(uu)::value, n = i + AHEAD;
-        if constexpr (n < N) op[n] = read_k(kt, kb0, n / 2, n % 2);
-        sn[i % 2] = mfma(op[i], qreg[i / 2], i < 2 ? f32x16{} : sn[i % 2]);
-      });
-      if (kind == 1) mask_scores<2>(sn, j0, hf, lim, a.sinks, there);
+      const unsigned vb0 = opaque(vbase);
+      auto scores = [&]() __attribute__((always_inline)) {
+        constexpr int N = 2 * (DH / 16), AHEAD = 3;
+        const unsigned kb0 = opaque(kbase);
+        bf16x8 op[N];
+        static_for<0, AHEAD>([&](auto uu) { constexpr int i = decltype(uu)::value; op[i] = read_k(kt, kb0, i / 2, i % 2); });
+        static_for<0, N>([&](auto uu) {
+          constexpr int i = decltype(uu)::value, n = i + AHEAD;
+          if constexpr (n < N) op[n] = read_k(kt, kb0, n / 2, n % 2);
+          sn[i % 2] = mfma(op[i], qreg[i / 2], i < 2 ? f32x16{} : sn[i % 2]);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if (kind == 1) mask_scores<2>(sn, j0, hf, lim, a.sinks, there);
+      };
+      scores();
       bf16x8 pp[2][2];
-      softmax<2, ND>(sn, pp, m_run, l_run, acc, a.sl2);
+      softmax<2, ND>(sn, scores, pp, m_run, l_run, acc, a.sl2);
       auto rd = [&](int db, int kb, int s2) __attribute__((always_inline)) { return read_v(vt, vb0, db, kb, s2); };
       if (kind == 1 && has_special<2, ND>(rd)) values_special<2, ND>(rd, pp, acc);
       else values<2, ND>(rd, pp, acc);
@@ -547,38 +602,249 @@ __global__ __launch_bounds__(kThreads, 2) void kv_tiles_kernel(KvAttnArgs a) {
     __builtin_amdgcn_s_waitcnt(kVmcnt0);
     __syncthreads();
   };
-  int u = u0;
-  for (; u + 1 < u1; u += 2) {
+#pragma unroll 1
+  for (int u = u0; u < u1; u += 2) {
     tile(IC<0>{}, u);
+    if (u + 1 >= u1) break;
     tile(IC<1>{}, u + 1);
   }
-  if (u < u1) tile(IC<0>{}, u);
 
-  if (w0 + l32 >= t.n_rows) return;
-  const float l = l_run + __shfl_xor(l_run, 32);
-  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-  const float l2 = l > 0.0f || l != l ? m_run + __log2f(l) : -INFINITY;
-  const long long row = (long long)(t.beg + tok) * a.Hq + hq;
-  if (a.npieces > 1) {
-    const long long at = (long long)z * a.s.n_tok * a.Hq + row;
-    if (hf == 0) a.part_lse[at] = l2;
-    if (u0 < u1) {
+  if (w0 + l32 < t.n_rows)
+    finish<DH>(a, z, (long long)(t.beg + tok) * a.Hq + hq, hf, u0 < u1, m_run, l_run, acc);
+}
+
+// ---------------------------------------------------------------------------
+// pairs
+// ---------------------------------------------------------------------------
+// 128-wide heads, many rows: 256 rows and eight waves per workgroup, one per compute unit.
+// Wave w runs on SIMD w mod 4, so every SIMD holds a wave of group A (0-3) and one of group
+// B (4-7).  The groups take turns, a barrier between: while one forms S of tile j and O of
+// tile j - 1 on the matrix core, the other does its softmax on the VALU.  B runs one
+// interval behind: in interval 2 j A multiplies for tile j and B takes the softmax of
+// j - 1, in 2 j + 1 A the softmax of j and B the products of j.  A fetches K[j + 1] at the
+// start of interval 2 j + 1, B V[j + 1] at the start of 2 j + 2, each into the buffer that
+// held tile j - 1, which no product of that interval reads.  (The tiles kernel leaves the
+// overlap of two workgroups to chance: matrix cores 30% busy, VALU 39%.)
+constexpr int kPairRows = 256, kPairThreads = 512;
+
+template <bool F8>
+__global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a) {
+  constexpr int DH = 128, CPR = DH / 8, ROWB = DH * 2, ND = DH / 32, TK = kTileKeys;
+  constexpr int C8 = DH / 16;                // 16-byte chunks of a row of codes
+  __shared__ __attribute__((aligned(1024))) uint16_t lds_k0[TK * DH];
+  __shared__ __attribute__((aligned(1024))) uint16_t lds_k1[TK * DH];
+  __shared__ __attribute__((aligned(1024))) uint16_t lds_v0[TK * DH];
+  __shared__ __attribute__((aligned(1024))) uint16_t lds_v1[TK * DH];
+  __shared__ __attribute__((aligned(1024))) uint16_t lds_zero[TK * DH];   // values of a tile that was not seen
+
+  int z, h;
+  RowTile t;
+  if (!my_unit<kPairRows, TK>(a, z, h, t)) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = wave >> 2, l32 = lane & 31, hf = lane >> 5;
+  int u0, u1;
+  piece_range(a, t.nt, z, u0, u1);
+
+  const int w0 = t.row0 + wave * 32;
+  const bool live = w0 < t.n_rows;
+  const int r = min(w0 + l32, t.n_rows - 1);
+  const int tok = r / a.g, hq = h * a.g + (r - tok * a.g);
+  const int p0 = t.off + min(w0, t.n_rows - 1) / a.g, p1 = t.off + min(w0 + 31, t.n_rows - 1) / a.g;
+  const RowLimits lim = row_limits(a, t, t.off + tok);
+  bf16x8 qreg[DH / 16];
+  {
+    const uint16_t* qp = a.q + (long long)(t.beg + tok) * a.qs + hq * DH + 8 * hf;
 #pragma unroll
-      for (int db = 0; db < ND; ++db)
-#pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4)
-          *reinterpret_cast<f32x4*>(a.part_o + at * DH + db * 32 + 8 * g4 + 4 * hf) =
-              f32x4{acc[db][4 * g4] * inv, acc[db][4 * g4 + 1] * inv, acc[db][4 * g4 + 2] * inv, acc[db][4 * g4 + 3] * inv};
-    }
-    return;
+    for (int i = 0; i < DH / 16; ++i) qreg[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qp + 16 * i));
   }
+
+  // ---- key lookup, as in the tiles kernel
+  const int32_t* table = a.s.table + (long long)t.b * a.s.max_pages;
+  auto tile_of = [&](int u) { return u < t.ts ? u : t.tw + (u - t.ts); };
+  struct Look { int key, id, rem; };
+  auto look = [&](int u) __attribute__((always_inline)) -> Look {
+    Look k;
+    k.key = tile_of(min(u, t.nt - 1)) * TK + lane;
+    const int kk = min(k.key, t.len - 1);
+    const int pg = div_by(kk, a.s.page);
+    k.id = table[pg];
+    k.rem = kk - pg * a.page;
+    return k;
+  };
+  const long long row_bytes = (long long)a.H * DH * (F8 ? 1 : 2), head_bytes = (long long)h * DH * (F8 ? 1 : 2);
+  int slot = 0, exp_at = 0;                  // of the lane's key: row of the cache; of codes page * H + h
+  auto resolve = [&](const Look& k, unsigned long long& there) __attribute__((always_inline)) {
+    const bool in = k.id >= 0 && k.id < a.pages;
+    there = __ballot(in && k.key < t.len);
+    slot = in ? k.id * a.page + k.rem : 0;
+    if (F8) exp_at = (in ? k.id : 0) * a.H + h;
+  };
+
+  // ---- a group's four waves copy a tile: bf16 straight into LDS, codes through registers
+  const int cw = wave & 3;
+  const int brow = cw * 4 + lane / CPR;
+  const int cofs = ((lane % CPR) ^ (grp == 0 ? kswz(brow, CPR) : vswz(brow, CPR))) * 16;
+  const uint8_t* src = (grp == 0 ? a.k : a.v) + head_bytes;
+  const uint8_t* exps = grp == 0 ? a.ke : a.ve;
+  auto copy_bf16 = [&](uint16_t* dst) __attribute__((always_inline)) {
+    static_for<0, 4>([&](auto rr) {
+      constexpr int i = decltype(rr)::value;
+      const long long at = (long long)__shfl(slot, brow + 16 * i) * row_bytes + cofs;
+      __builtin_amdgcn_global_load_lds((glb_void*)(src + at), (lds_void*)(reinterpret_cast<char*>(dst) + (cw + 4 * i) * 1024), 16, 0, 0);
+    });
+  };
+  u32x4 code[2];
+  int ex = 0;
+  const int tg = tid & 255;
+  auto load8 = [&]() __attribute__((always_inline)) {
+    ex = exps[exp_at];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = tg + 256 * i;
+      code[i] = *reinterpret_cast<const u32x4*>(src + (long long)__shfl(slot, c / C8) * row_bytes + (c % C8) * 16);
+    }
+  };
+  auto store8 = [&](uint16_t* dst) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = tg + 256 * i, row = c / C8, ch = 2 * (c % C8);
+      const float sc = byte_scale(__shfl(ex, row));
+      const int sw = grp == 0 ? kswz(row, CPR) : vswz(row, CPR);
+      char* at = reinterpret_cast<char*>(dst) + row * ROWB;
+      *reinterpret_cast<u32x4*>(at + ((ch ^ sw) * 16)) = widen8(code[i].x, code[i].y, sc);
+      *reinterpret_cast<u32x4*>(at + (((ch + 1) ^ sw) * 16)) = widen8(code[i].z, code[i].w, sc);
+    }
+  };
+
+  // ---- LDS reads (bytes within a tile); see kswz, vswz
+  const unsigned kbase = (unsigned)(l32 * ROWB + ((hf ^ kswz(l32, CPR)) * 16));
+  unsigned vbase;
+  {
+    const int gq = lane >> 4, la = lane & 15;
+    const int vr = 4 * (gq >> 1) + (la >> 2);
+    const int c = 2 * (gq & 1) + ((la & 3) >> 1);
+    vbase = (unsigned)(vr * ROWB + ((c ^ vswz(vr, CPR)) * 16) + 8 * (la & 1));
+  }
+  auto opaque = [](unsigned x) { asm volatile("" : "+v"(x)); return x; };
+  auto read_k = [&](const uint16_t* kt, unsigned kb0, int i, int kb) __attribute__((always_inline)) -> bf16x8 {
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(
+        reinterpret_cast<const char*>(kt) + (kb0 ^ (32u * i)) + kb * 32 * ROWB));
+  };
+  auto read_v = [&](const uint16_t* vt, unsigned vb0, int db, int kb, int s2) __attribute__((always_inline)) -> bf16x8 {
+    const lds_char* p = (const lds_char*)(vt) + (vb0 ^ (64u * db)) + (32 * kb + 16 * s2) * ROWB;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * ROWB)));
+    return __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+  };
+
+  f32x16 acc[ND];
 #pragma unroll
   for (int db = 0; db < ND; ++db)
 #pragma unroll
-    for (int g4 = 0; g4 < 4; ++g4)
-      put4(a, row, DH, db * 32 + 8 * g4 + 4 * hf,
-           f32x4{acc[db][4 * g4] * inv, acc[db][4 * g4 + 1] * inv, acc[db][4 * g4 + 2] * inv, acc[db][4 * g4 + 3] * inv});
-  if (a.lse != nullptr && hf == 0) a.lse[row] = l2 * kLn2;
+    for (int e = 0; e < 16; ++e) acc[db][e] = 0.0f;
+  f32x16 sn[2];
+  bf16x8 pp[2][2];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) pp[g / 2][g % 2] = bf16x8{};
+  float m_run = kNoMax, l_run = 0.0f;
+  bool has_p = false;                        // pp holds a tile whose products are to come
+
+  // ---- S of tile j and O of tile j - 1, one MFMA of each per step, operands read three
+  //      steps ahead; step i: S chain i % 2, channels 16 (i / 2); O block i % 4, keys
+  //      (kb, s2) = (i / 8, (i / 4) % 2)
+  auto products = [&](const uint16_t* kt, const uint16_t* vt, auto with_o) __attribute__((always_inline)) {
+    constexpr bool O = decltype(with_o)::value != 0;
+    constexpr int N = 16, AHEAD = 3;
+    const unsigned kb0 = opaque(kbase), vb0 = opaque(vbase);
+    bf16x8 opk[N], opv[N];
+    auto rd = [&](auto uu) __attribute__((always_inline)) {
+      constexpr int i = decltype(uu)::value;
+      opk[i] = read_k(kt, kb0, i / 2, i % 2);
+      if constexpr (O) opv[i] = read_v(vt, vb0, i % ND, i / (2 * ND), (i / ND) % 2);
+    };
+    static_for<0, AHEAD>([&](auto i) { rd(i); });
+    static_for<0, N>([&](auto uu) {
+      constexpr int i = decltype(uu)::value;
+      if constexpr (i + AHEAD < N) rd(IC<i + AHEAD>{});
+      sn[i % 2] = mfma(opk[i], qreg[i / 2], i < 2 ? f32x16{} : sn[i % 2]);
+      if constexpr (O) acc[i % ND] = mfma(opv[i], pp[i / (2 * ND)][(i / ND) % 2], acc[i % ND]);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+
+  const int n = u1 - u0;
+  unsigned long long there = 0, there_next = 0;
+  Look nxt{};
+  if (n > 0) {
+    for (int x = tid; x < TK * DH / 8; x += kPairThreads) reinterpret_cast<u32x4*>(lds_zero)[x] = u32x4{0u, 0u, 0u, 0u};
+    resolve(look(u0), there);
+    if constexpr (F8) {
+      load8();
+      store8(grp == 0 ? lds_k0 : lds_v0);
+    } else {
+      copy_bf16(grp == 0 ? lds_k0 : lds_v0);
+    }
+    nxt = look(u0 + 1);
+    __builtin_amdgcn_s_waitcnt(kVmcnt0);
+    __syncthreads();
+    if (grp == 1) __syncthreads();
+    auto step = [&](auto par, int j) __attribute__((always_inline)) {
+      constexpr int P = decltype(par)::value;
+      const uint16_t* kc = P == 0 ? lds_k0 : lds_k1;     // K[j]
+      const uint16_t* vc = P == 0 ? lds_v0 : lds_v1;     // V[j]
+      uint16_t* kn = P == 0 ? lds_k1 : lds_k0;           // K[j - 1], then K[j + 1]
+      uint16_t* vn = P == 0 ? lds_v1 : lds_v0;           // V[j - 1], then V[j + 1]
+      const int j0 = tile_of(u0 + j) * TK;
+      const int kind = live && j < n ? tile_kind<TK>(a, j0, p0, p1, there) : 0;
+      // (one path for both products: with a path for each case the accumulators moved between
+      // registers; a product that is not wanted meets zeros or is not looked at)
+      if (kind != 0 || has_p) products(kc, has_p ? vn : lds_zero, IC<1>{});
+      has_p = kind != 0;
+      __syncthreads();
+      const bool more = j + 1 < n;
+      if (more) {
+        resolve(nxt, there_next);
+        if constexpr (F8) load8();
+        else copy_bf16(grp == 0 ? kn : vn);
+        nxt = look(u0 + j + 2);
+      }
+      if (kind != 0) {
+        auto mask = [&]() __attribute__((always_inline)) {
+          if (kind == 1) mask_scores<2>(sn, j0, hf, lim, a.sinks, there);
+        };
+        mask();
+        softmax<2, ND>(sn, [&]() __attribute__((always_inline)) {
+          products(kc, vc, IC<0>{});                     // K[j] is still there
+          mask();
+        }, pp, m_run, l_run, acc, a.sl2);
+        if (kind == 1) {
+          const unsigned vb0 = opaque(vbase);
+          auto rd = [&](int db, int kb, int s2) __attribute__((always_inline)) { return read_v(vc, vb0, db, kb, s2); };
+          if (has_special<2, ND>(rd)) {
+            values_special<2, ND>(rd, pp, acc);
+            has_p = false;
+          }
+        }
+      }
+      if constexpr (F8) {
+        if (more) store8(grp == 0 ? kn : vn);
+      }
+      there = there_next;
+      // (the barrier's fence does not wait for copies into LDS)
+      __builtin_amdgcn_s_waitcnt(kVmcnt0);
+      __syncthreads();
+    };
+#pragma unroll 1
+    for (int j = 0; j <= n; j += 2) {
+      step(IC<0>{}, j);
+      if (j + 1 > n) break;
+      step(IC<1>{}, j + 1);
+    }
+    if (grp == 0) __syncthreads();           // B's extra interval at the start
+  }
+  if (w0 + l32 < t.n_rows)
+    finish<DH>(a, z, (long long)(t.beg + tok) * a.Hq + hq, hf, n > 0, m_run, l_run, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -908,7 +1174,10 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
       if (kind == 1) {
         uint32_t m = 0;
 #pragma unroll
-        for (int db = 0; db < ND; ++db) m |= special_bits(read_v(vrd, db));
+        for (int db = 0; db < ND; ++db) {
+          m |= special_bits(read_v(vrd, db));
+          PIN(m);
+        }
         special = __ballot((m & 0x80008000u) != 0) != 0ull;
       }
       // (special tiles fetch the next values later: together with them they need more registers)
@@ -924,13 +1193,15 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
       } else {
 #pragma unroll
         for (int db = 0; db < ND; ++db) {
-          const Images v = images(read_v(vrd, db));
+          const bf16x8 op = read_v(vrd, db);
 #pragma unroll
           for (int nq = 0; nq < NQ; ++nq) {
             const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
             const bf16x8 w = seen_weights(pp[nq][sub]);
-            acc[nq][db] = mfma16(v.fin, pp[nq][sub], acc[nq][db]);
-            add_special<4>(acc[nq][db], mfma16(v.pos, w, zero), mfma16(v.neg, w, zero));
+            acc[nq][db] = mfma16(part_of<kFinite>(op), pp[nq][sub], acc[nq][db]);
+            add_infinity<4>(acc[nq][db], mfma16(part_of<kPlus>(op), w, zero), 1.0f);
+            add_infinity<4>(acc[nq][db], mfma16(part_of<kMinus>(op), w, zero), -1.0f);
+            PIN(acc[nq][db]);
           }
         }
         if (more) load_rows(a.v, at, vr, 2 * sub, 2 * sub + 2);
@@ -1097,7 +1368,13 @@ template <int DH, bool F8>
 void launch_as(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
   if (p.rows == 16) return launch_rows<DH, F8, 1>(a, p, stream);
   if (p.rows == 32) return launch_rows<DH, F8, 2>(a, p, stream);
-  hipLaunchKernelGGL((kv_tiles_kernel<DH, F8>), dim3(p.row_tiles * a.H * p.pieces), dim3(kThreads), 0, stream, a);
+  const dim3 grid(p.row_tiles * a.H * p.pieces);
+  if constexpr (DH == 128) {
+    if (p.rows == kPairRows) hipLaunchKernelGGL((kv_pairs_kernel<F8>), grid, dim3(kPairThreads), 0, stream, a);
+    else hipLaunchKernelGGL((kv_tiles_kernel<DH, F8>), grid, dim3(kThreads), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((kv_tiles_kernel<DH, F8>), grid, dim3(kThreads), 0, stream, a);
+  }
   if (p.pieces > 1) {
     const long long threads = (long long)a.s.n_tok * a.Hq * (DH / 4);
     hipLaunchKernelGGL((kv_join_kernel<DH>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
@@ -1111,7 +1388,7 @@ KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f
                         int cus) {
   KvAttnPlan p{};
   const long long rows = n_tok * g, mean = (rows + n_seq - 1) / n_seq;
-  p.rows = mean <= 16 ? 16 : mean <= 64 ? 32 : kTileRows;
+  p.rows = mean <= 16 ? 16 : mean <= 64 ? 32 : dh < 128 || mean <= kTileRows ? kTileRows : kPairRows;
   p.wh = H % 4 == 0 ? 4 : H % 2 == 0 ? 2 : 1;
   p.row_tiles = (int)(rows / p.rows + n_seq);
   p.pieces = 1;
@@ -1132,7 +1409,7 @@ KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f
     return p;
   }
   const long long units = tiles * H, nt = (keys + kTileKeys - 1) / kTileKeys;
-  const long long want = (long long)cus * 2 / std::max(units, 1ll);
+  const long long want = (long long)cus * (p.rows == kPairRows ? 1 : 2) / std::max(units, 1ll);
   const long long most = std::min<long long>(std::min<long long>(want, kMaxPieces), (nt + 7) / 8);   // 8 key tiles at least
   if (most < 2) return p;
   p.piece_tiles = (int)((nt + most - 1) / most);
