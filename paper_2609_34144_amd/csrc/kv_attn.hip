@@ -192,17 +192,31 @@ __device__ __forceinline__ RowLimits row_limits(const KvAttnArgs& a, const RowTi
 }
 
 // Whether a key tile [j0, j0 + TK) is seen by none (0), some (1) or all (2) of the rows at
-// positions p0 .. p1; `there`: bit per key, set where the key exists.
-template <int TK>
-__device__ __forceinline__ int tile_kind(const KvAttnArgs& a, int j0, int p0, int p1, unsigned long long there) {
-  const unsigned long long all = TK == 64 ? ~0ull : (1ull << TK) - 1;
-  if (there == 0) return 0;
-  if (a.causal && j0 > p1) return 0;
-  const bool win = a.window > 0;
-  if (win && j0 + TK - 1 <= p0 - a.window && j0 >= a.sinks) return 0;
-  const bool full = there == all && (!a.causal || j0 + TK - 1 <= p0) &&
-                    (!win || j0 > p1 - a.window || j0 + TK - 1 < a.sinks);
-  return full ? 2 : 1;
+// positions p0 .. p1; `there`: BITS bits, set where the keys exist.  Sign bits instead of
+// comparisons: branches would cut up the products beside which this is worked out.
+struct KindBounds {
+  int c0, c1;                    // the last key that row p0, row p1 sees
+  int w0, w1;                    // the last key before their windows
+  int sinks;
+};
+__device__ __forceinline__ KindBounds kind_bounds(const KvAttnArgs& a, int len, int p0, int p1) {
+  const int far = 1 << 30;       // (positions, lengths and windows are at most that)
+  return KindBounds{a.causal ? min(p0, len - 1) : len - 1, a.causal ? min(p1, len - 1) : len - 1, a.window > 0 ? max(p0 - a.window, -1) : -1,
+                    a.window > 0 ? max(p1 - a.window, -1) : -1, min(a.sinks, far)};
+}
+__device__ __forceinline__ int less(int x, int y) { return (int)((unsigned)(x - y) >> 31); }   // 1 where x < y
+template <int TK, int BITS = TK>
+__device__ __forceinline__ int tile_kind(const KindBounds& k, int j0, unsigned long long there) {
+  const int last = j0 + TK - 1, n = (int)__popcll(there);
+  const int none = less(n, 1) | less(k.c1, j0) | (less(last, k.w0 + 1) & less(k.sinks, j0 + 1));
+  const int full = less(BITS - 1, n) & less(last, k.c0 + 1) & (less(k.w1, j0) | less(last, k.sinks));
+  return (1 + full) & (none - 1);
+}
+
+// a byte of ones for each of eight bits
+__device__ __forceinline__ unsigned long long bytes_of(unsigned long long bits) {
+  const unsigned long long x = (bits * 0x0101010101010101ull) & 0x8040201008040201ull;
+  return (((x + 0x7f7f7f7f7f7f7f7full) >> 7) & 0x0101010101010101ull) * 0xff;
 }
 
 // The lane's visible keys among j0 .. j0 + 31 as bits (of those in `there`).
@@ -413,7 +427,14 @@ __device__ __forceinline__ void finish(const KvAttnArgs& a, int z, long long row
 // ---------------------------------------------------------------------------
 // tiles
 // ---------------------------------------------------------------------------
-template <int DH, bool F8>
+// RUNS (both tiles kernels): pages of a multiple of copy_rows(DH) tokens.  Then the rows of
+// one copy instruction of a wave, which start at a multiple of it, lie side by side in one
+// page, and their place is one number for the wave; else every lane fetches its row's place
+// from the lane that looked it up.  (28160 keys, 4 x 3520 rows of 24 heads of 128: XX us
+// so, 5008 us with the places passed between lanes: the LDS, which that goes through, is as
+// busy as the matrix cores.)
+constexpr int copy_rows(int dh) { return 1024 / dh; }
+template <int DH, bool F8, bool RUNS>
 __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv_tiles_kernel(KvAttnArgs a) {
   constexpr int CPR = DH / 8, ROWB = DH * 2, ND = DH / 32, TK = kTileKeys;
   constexpr int NSLOT = DH / 32;             // 1-KB copies of a bf16 tile per wave
@@ -442,6 +463,7 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
   const int tok = r / a.g, hq = h * a.g + (r - tok * a.g);
   const int p0 = t.off + min(w0, t.n_rows - 1) / a.g, p1 = t.off + min(w0 + 31, t.n_rows - 1) / a.g;
   const RowLimits lim = row_limits(a, t, t.off + tok);
+  const KindBounds kb = kind_bounds(a, t.len, p0, p1);
   bf16x8 qreg[DH / 16];
   {
     const uint16_t* qp = a.q + (long long)(t.beg + tok) * a.qs + hq * DH + 8 * hf;
@@ -456,7 +478,9 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
   auto look = [&](int u) __attribute__((always_inline)) -> Look {
     Look k;
     k.key = tile_of(min(u, t.nt - 1)) * TK + lane;
-    const int kk = min(k.key, t.len - 1);
+    // (RUNS: a run past the end stands in for itself from the last key's run)
+    const int kk = RUNS ? (k.key < t.len ? k.key : ((t.len - 1) & -copy_rows(DH)) + (k.key & (copy_rows(DH) - 1)))
+                        : min(k.key, t.len - 1);
     const int pg = div_by(kk, a.s.page);
     k.id = table[pg];
     k.rem = kk - pg * a.page;
@@ -476,10 +500,19 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
   auto copy_bf16 = [&](int slot, uint16_t* kd, uint16_t* vd) __attribute__((always_inline)) {
     static_for<0, NSLOT>([&](auto rr) {
       constexpr int i = decltype(rr)::value;
-      const long long at = (long long)__shfl(slot, brow + i * RSTEP) * row_bytes + head_bytes;
       const int lb = (wave + 4 * i) * 1024;
-      __builtin_amdgcn_global_load_lds((glb_void*)(a.k + at + kofs), (lds_void*)(reinterpret_cast<char*>(kd) + lb), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((glb_void*)(a.v + at + vofs), (lds_void*)(reinterpret_cast<char*>(vd) + lb), 16, 0, 0);
+      const uint8_t *kp, *vp;
+      if constexpr (RUNS) {
+        const long long at = (long long)__builtin_amdgcn_readlane(slot, wave * (512 / DH) + i * RSTEP) * row_bytes + head_bytes;
+        kp = a.k + at + (unsigned)(lane / CPR * (int)row_bytes + kofs);
+        vp = a.v + at + (unsigned)(lane / CPR * (int)row_bytes + vofs);
+      } else {
+        const long long at = (long long)__shfl(slot, brow + i * RSTEP) * row_bytes + head_bytes;
+        kp = a.k + at + kofs;
+        vp = a.v + at + vofs;
+      }
+      __builtin_amdgcn_global_load_lds((glb_void*)kp, (lds_void*)(reinterpret_cast<char*>(kd) + lb), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((glb_void*)vp, (lds_void*)(reinterpret_cast<char*>(vd) + lb), 16, 0, 0);
     });
   };
   u32x4 ck[N8], cv[N8];
@@ -490,7 +523,13 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
 #pragma unroll
     for (int i = 0; i < N8; ++i) {
       const int c = tid + i * kThreads, row = min(c / C8, TK - 1);
-      const long long at = (long long)__shfl(slot, row) * row_bytes + head_bytes + (c % C8) * 16;
+      long long at = head_bytes;
+      if constexpr (RUNS) {
+        const int first = min(wave * (64 / C8) + i * (kThreads / C8), TK - 1);
+        at += (long long)__builtin_amdgcn_readlane(slot, first) * row_bytes + (unsigned)(lane / C8 * (int)row_bytes + (lane % C8) * 16);
+      } else {
+        at += (long long)__shfl(slot, row) * row_bytes + (c % C8) * 16;
+      }
       ck[i] = *reinterpret_cast<const u32x4*>(a.k + at);
       cv[i] = *reinterpret_cast<const u32x4*>(a.v + at);
     }
@@ -499,7 +538,9 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
 #pragma unroll
     for (int i = 0; i < N8; ++i) {
       const int c = tid + i * kThreads, row = c / C8, ch = 2 * (c % C8);
-      const int e = __shfl(ex, min(row, TK - 1));
+      int e;
+      if constexpr (RUNS) e = __builtin_amdgcn_readlane(ex, min(wave * (64 / C8) + i * (kThreads / C8), TK - 1));
+      else e = __shfl(ex, min(row, TK - 1));
       if (row < TK) {
         const float sk = byte_scale(e & 255), sv = byte_scale(e >> 8);
         char* kr = reinterpret_cast<char*>(kd) + row * ROWB;
@@ -571,7 +612,7 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
       nxt = look(u + 2);
     }
     const int j0 = tile_of(u) * TK;
-    const int kind = live ? tile_kind<TK>(a, j0, p0, p1, there) : 0;
+    const int kind = live ? tile_kind<TK>(kb, j0, there) : 0;
     if (kind != 0) {
       f32x16 sn[2];
       const unsigned vb0 = opaque(vbase);
@@ -627,7 +668,7 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
 // overlap of two workgroups to chance: matrix cores 30% busy, VALU 39%.)
 constexpr int kPairRows = 256, kPairThreads = 512;
 
-template <bool F8>
+template <bool F8, bool RUNS>
 __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a) {
   constexpr int DH = 128, CPR = DH / 8, ROWB = DH * 2, ND = DH / 32, TK = kTileKeys;
   constexpr int C8 = DH / 16;                // 16-byte chunks of a row of codes
@@ -652,6 +693,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
   const int tok = r / a.g, hq = h * a.g + (r - tok * a.g);
   const int p0 = t.off + min(w0, t.n_rows - 1) / a.g, p1 = t.off + min(w0 + 31, t.n_rows - 1) / a.g;
   const RowLimits lim = row_limits(a, t, t.off + tok);
+  const KindBounds kb = kind_bounds(a, t.len, p0, p1);
   bf16x8 qreg[DH / 16];
   {
     const uint16_t* qp = a.q + (long long)(t.beg + tok) * a.qs + hq * DH + 8 * hf;
@@ -666,7 +708,9 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
   auto look = [&](int u) __attribute__((always_inline)) -> Look {
     Look k;
     k.key = tile_of(min(u, t.nt - 1)) * TK + lane;
-    const int kk = min(k.key, t.len - 1);
+    // (RUNS: a run past the end stands in for itself from the last key's run)
+    const int kk = RUNS ? (k.key < t.len ? k.key : ((t.len - 1) & -copy_rows(DH)) + (k.key & (copy_rows(DH) - 1)))
+                        : min(k.key, t.len - 1);
     const int pg = div_by(kk, a.s.page);
     k.id = table[pg];
     k.rem = kk - pg * a.page;
@@ -681,35 +725,75 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
     if (F8) exp_at = (in ? k.id : 0) * a.H + h;
   };
 
+  // With RUNS one lookup serves eight tiles: lane l looks up the run of eight keys
+  // l mod 8 of tile l / 8 of a window of them, and keeps its address.  (Looked up tile by
+  // tile, a tile cost 55 more vector and 55 more scalar instructions than the products and
+  // the softmax take, 28160 keys of 4 x 3520 rows 4856 us for XX.)
+  constexpr int GR = copy_rows(DH), GPT = TK / GR, TPW = 64 / GPT;
+  static_assert(GPT == 8, "eight runs per tile: a byte of the window's mask");
+  int win_id = 0, win_rem = 0;               // the next window's lookup
+  unsigned run_lo = 0, run_hi = 0;           // this window's addresses
+  unsigned long long runs = 0;               // which of its runs exist
+  auto open_window = [&](int u) __attribute__((always_inline)) {
+    const int key = tile_of(min(u + lane / GPT, t.nt - 1)) * TK + lane % GPT * GR;
+    const int kk = key < t.len ? key : (t.len - 1) & -GR;
+    const int pg = div_by(kk, a.s.page);
+    win_id = table[pg];
+    win_rem = kk - pg * a.page;
+  };
+
   // ---- a group's four waves copy a tile: bf16 straight into LDS, codes through registers
   const int cw = wave & 3;
   const int brow = cw * 4 + lane / CPR;
   const int cofs = ((lane % CPR) ^ (grp == 0 ? kswz(brow, CPR) : vswz(brow, CPR))) * 16;
   const uint8_t* src = (grp == 0 ? a.k : a.v) + head_bytes;
   const uint8_t* exps = grp == 0 ? a.ke : a.ve;
-  auto copy_bf16 = [&](uint16_t* dst) __attribute__((always_inline)) {
+  const int tg = tid & 255;
+  int ex = 0;                                // codes: exponent byte of the lane's key or run
+  auto enter_window = [&]() __attribute__((always_inline)) {
+    const bool in = win_id >= 0 && win_id < a.pages;
+    runs = __ballot(in);
+    const uint8_t* at = src + (long long)(in ? win_id * a.page + win_rem : 0) * row_bytes;
+    run_lo = (unsigned)(unsigned long long)at;
+    run_hi = (unsigned)((unsigned long long)at >> 32);
+    if (F8) ex = exps[(in ? win_id : 0) * a.H + h];
+  };
+  // run (in its tile) of a wave's copy i, and the lane's place from there
+  auto run_of = [&](int i) { return F8 ? cw + 4 * i : 2 * i + (cw >> 1); };
+  const unsigned lane_at = F8 ? (unsigned)(lane / C8 * (int)row_bytes + lane % C8 * 16)
+                              : (unsigned)(((cw & 1) * 4 + lane / CPR) * (int)row_bytes + cofs);
+  auto opaque = [](unsigned x) { asm volatile("" : "+v"(x)); return x; };
+  auto place = [&](int i, int wt) __attribute__((always_inline)) -> const uint8_t* {   // wt: tile of the window
+    if constexpr (RUNS) {
+      const int l = wt * GPT + run_of(i);
+      const unsigned long long at = (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)run_hi, l) << 32 |
+                                    (unsigned)__builtin_amdgcn_readlane((int)run_lo, l);
+      return reinterpret_cast<const uint8_t*>(at) + opaque(lane_at);   // (opaque: scalar base + lane offset)
+    } else {
+      const int c = tg + 256 * i;
+      return src + (long long)__shfl(slot, F8 ? c / C8 : brow + 16 * i) * row_bytes + (F8 ? c % C8 * 16 : cofs);
+    }
+  };
+  auto copy_bf16 = [&](uint16_t* dst, int wt) __attribute__((always_inline)) {
     static_for<0, 4>([&](auto rr) {
       constexpr int i = decltype(rr)::value;
-      const long long at = (long long)__shfl(slot, brow + 16 * i) * row_bytes + cofs;
-      __builtin_amdgcn_global_load_lds((glb_void*)(src + at), (lds_void*)(reinterpret_cast<char*>(dst) + (cw + 4 * i) * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((glb_void*)place(i, wt), (lds_void*)(reinterpret_cast<char*>(dst) + (cw + 4 * i) * 1024), 16, 0, 0);
     });
   };
   u32x4 code[2];
-  int ex = 0;
-  const int tg = tid & 255;
-  auto load8 = [&]() __attribute__((always_inline)) {
-    ex = exps[exp_at];
+  auto load8 = [&](int wt) __attribute__((always_inline)) {
+    if (!RUNS) ex = exps[exp_at];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int c = tg + 256 * i;
-      code[i] = *reinterpret_cast<const u32x4*>(src + (long long)__shfl(slot, c / C8) * row_bytes + (c % C8) * 16);
-    }
+    for (int i = 0; i < 2; ++i) code[i] = *reinterpret_cast<const u32x4*>(place(i, wt));
   };
-  auto store8 = [&](uint16_t* dst) __attribute__((always_inline)) {
+  auto store8 = [&](uint16_t* dst, int wt) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int c = tg + 256 * i, row = c / C8, ch = 2 * (c % C8);
-      const float sc = byte_scale(__shfl(ex, row));
+      int e;
+      if constexpr (RUNS) e = __builtin_amdgcn_readlane(ex, wt * GPT + run_of(i));
+      else e = __shfl(ex, row);
+      const float sc = byte_scale(e);
       const int sw = grp == 0 ? kswz(row, CPR) : vswz(row, CPR);
       char* at = reinterpret_cast<char*>(dst) + row * ROWB;
       *reinterpret_cast<u32x4*>(at + ((ch ^ sw) * 16)) = widen8(code[i].x, code[i].y, sc);
@@ -726,7 +810,6 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
     const int c = 2 * (gq & 1) + ((la & 3) >> 1);
     vbase = (unsigned)(vr * ROWB + ((c ^ vswz(vr, CPR)) * 16) + 8 * (la & 1));
   }
-  auto opaque = [](unsigned x) { asm volatile("" : "+v"(x)); return x; };
   auto read_k = [&](const uint16_t* kt, unsigned kb0, int i, int kb) __attribute__((always_inline)) -> bf16x8 {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(
         reinterpret_cast<const char*>(kt) + (kb0 ^ (32u * i)) + kb * 32 * ROWB));
@@ -752,11 +835,11 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
 
   // ---- S of tile j and O of tile j - 1, one MFMA of each per step, operands read three
   //      steps ahead; step i: S chain i % 2, channels 16 (i / 2); O block i % 4, keys
-  //      (kb, s2) = (i / 8, (i / 4) % 2)
-  auto products = [&](const uint16_t* kt, const uint16_t* vt, auto with_o) __attribute__((always_inline)) {
+  //      (kb, s2) = (i / 8, (i / 4) % 2).  also(i) is issued beside step i.
+  auto products = [&](const uint16_t* kt, const uint16_t* vt, auto with_o, auto&& also) __attribute__((always_inline)) {
     constexpr bool O = decltype(with_o)::value != 0;
     constexpr int N = 16, AHEAD = 3;
-    const unsigned kb0 = opaque(kbase), vb0 = opaque(vbase);
+    const unsigned kb0 = kbase, vb0 = vbase;
     bf16x8 opk[N], opv[N];
     auto rd = [&](auto uu) __attribute__((always_inline)) {
       constexpr int i = decltype(uu)::value;
@@ -769,26 +852,40 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
       if constexpr (i + AHEAD < N) rd(IC<i + AHEAD>{});
       sn[i % 2] = mfma(opk[i], qreg[i / 2], i < 2 ? f32x16{} : sn[i % 2]);
       if constexpr (O) acc[i % ND] = mfma(opv[i], pp[i / (2 * ND)][(i / ND) % 2], acc[i % ND]);
+      also(uu);
       __builtin_amdgcn_sched_barrier(0);
     });
   };
 
   const int n = u1 - u0;
+  // keys of tile j that exist, and of the next: bits per key, with RUNS per run
   unsigned long long there = 0, there_next = 0;
   Look nxt{};
+  auto fetch = [&](uint16_t* kd, uint16_t* vd, int wt) __attribute__((always_inline)) {
+    if constexpr (F8) load8(wt);
+    else copy_bf16(grp == 0 ? kd : vd, wt);
+  };
+  auto runs_of = [&](int wt) { return (runs >> (wt * GPT)) & 0xff; };
   if (n > 0) {
     for (int x = tid; x < TK * DH / 8; x += kPairThreads) reinterpret_cast<u32x4*>(lds_zero)[x] = u32x4{0u, 0u, 0u, 0u};
-    resolve(look(u0), there);
-    if constexpr (F8) {
-      load8();
-      store8(grp == 0 ? lds_k0 : lds_v0);
+    if constexpr (RUNS) {
+      open_window(u0);
+      enter_window();
+      open_window(u0 + TPW);
+      there = runs_of(0);
     } else {
-      copy_bf16(grp == 0 ? lds_k0 : lds_v0);
+      resolve(look(u0), there);
     }
-    nxt = look(u0 + 1);
+    fetch(lds_k0, lds_v0, 0);
+    if constexpr (F8) store8(grp == 0 ? lds_k0 : lds_v0, 0);
+    if constexpr (!RUNS) nxt = look(u0 + 1);
     __builtin_amdgcn_s_waitcnt(kVmcnt0);
     __syncthreads();
     if (grp == 1) __syncthreads();
+    auto kind_of = [&](int j, unsigned long long th) __attribute__((always_inline)) {
+      return -((int)live & less(j, n)) & tile_kind<TK, RUNS ? GPT : TK>(kb, tile_of(u0 + j) * TK, th);
+    };
+    int kind = kind_of(0, there), kind_next = 0;
     auto step = [&](auto par, int j) __attribute__((always_inline)) {
       constexpr int P = decltype(par)::value;
       const uint16_t* kc = P == 0 ? lds_k0 : lds_k1;     // K[j]
@@ -796,26 +893,39 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
       uint16_t* kn = P == 0 ? lds_k1 : lds_k0;           // K[j - 1], then K[j + 1]
       uint16_t* vn = P == 0 ? lds_v1 : lds_v0;           // V[j - 1], then V[j + 1]
       const int j0 = tile_of(u0 + j) * TK;
-      const int kind = live && j < n ? tile_kind<TK>(a, j0, p0, p1, there) : 0;
+      const int wt = (j + 1) % TPW;                      // tile j + 1 in its window
+      // What tile j + 1 needs to know is worked out beside the products, where the wave waits
+      // for the matrix core anyway.
+      auto prepare = [&](auto uu) __attribute__((always_inline)) {
+        constexpr int i = decltype(uu)::value;
+        if constexpr (!RUNS && i == 1) resolve(nxt, there_next);
+        if constexpr (!RUNS && i == 5) nxt = look(u0 + j + 2);
+        if constexpr (RUNS && i == 5) there_next = runs_of(wt);
+        if constexpr (i == 9) kind_next = kind_of(j + 1, there_next);
+      };
+      if constexpr (RUNS) {
+        if (wt == 0) {                                   // (the copies of tile j are done)
+          enter_window();
+          open_window(u0 + j + 1 + TPW);
+        }
+      }
       // (one path for both products: with a path for each case the accumulators moved between
       // registers; a product that is not wanted meets zeros or is not looked at)
-      if (kind != 0 || has_p) products(kc, has_p ? vn : lds_zero, IC<1>{});
+      if (kind != 0 || has_p) products(kc, has_p ? vn : lds_zero, IC<1>{}, prepare);
+      else static_for<0, 16>(prepare);
       has_p = kind != 0;
       __syncthreads();
       const bool more = j + 1 < n;
-      if (more) {
-        resolve(nxt, there_next);
-        if constexpr (F8) load8();
-        else copy_bf16(grp == 0 ? kn : vn);
-        nxt = look(u0 + j + 2);
-      }
+      if (more) fetch(kn, vn, wt);
       if (kind != 0) {
         auto mask = [&]() __attribute__((always_inline)) {
-          if (kind == 1) mask_scores<2>(sn, j0, hf, lim, a.sinks, there);
+          if (kind == 1) mask_scores<2>(sn, j0, hf, lim, a.sinks, RUNS ? bytes_of(there) : there);
         };
         mask();
+        PIN(sn[0]);
+        PIN(sn[1]);
         softmax<2, ND>(sn, [&]() __attribute__((always_inline)) {
-          products(kc, vc, IC<0>{});                     // K[j] is still there
+          products(kc, vc, IC<0>{}, [](auto) {});        // K[j] is still there
           mask();
         }, pp, m_run, l_run, acc, a.sl2);
         if (kind == 1) {
@@ -828,9 +938,10 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
         }
       }
       if constexpr (F8) {
-        if (more) store8(grp == 0 ? kn : vn);
+        if (more) store8(grp == 0 ? kn : vn, wt);
       }
       there = there_next;
+      kind = kind_next;
       // (the barrier's fence does not wait for copies into LDS)
       __builtin_amdgcn_s_waitcnt(kVmcnt0);
       __syncthreads();
@@ -966,6 +1077,7 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
   const int u0 = min(it.z * it.per, t.nt), u1 = min(u0 + min(it.per, t.nt), t.nt);
   const int nrows = min(TM, t.n_rows - t.row0);
   const int p0 = t.off + t.row0 / a.g, p1 = t.off + (t.row0 + nrows - 1) / a.g;
+  const KindBounds kb = kind_bounds(a, t.len, p0, p1);
   RowLimits lim[NQ];
   bf16x8 qreg[NQ][NT];
 #pragma unroll
@@ -1109,7 +1221,7 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
 #pragma unroll
       for (int r = 0; r < R; ++r) ve_cur[r] = ve[r];
     }
-    const int kind = tile_kind<TK>(a, j0, p0, p1, there);
+    const int kind = tile_kind<TK>(kb, j0, there);
     if (more) {
       resolve(nxt, there_next);
       load_rows(a.k, at, kr, 0, R);
@@ -1364,17 +1476,24 @@ void launch_rows(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
     hipLaunchKernelGGL((kv_rows_join_kernel<DH, 16 * NQ>), dim3(p.row_tiles, a.H, 16 * NQ), dim3(kThreads), 0, stream, a);
 }
 
+template <int DH, bool F8, bool RUNS>
+void launch_tiles(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
+  const dim3 grid(p.row_tiles * a.H * p.pieces);
+  if constexpr (DH == 128) {
+    if (p.rows == kPairRows) {
+      hipLaunchKernelGGL((kv_pairs_kernel<F8, RUNS>), grid, dim3(kPairThreads), 0, stream, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((kv_tiles_kernel<DH, F8, RUNS>), grid, dim3(kThreads), 0, stream, a);
+}
+
 template <int DH, bool F8>
 void launch_as(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
   if (p.rows == 16) return launch_rows<DH, F8, 1>(a, p, stream);
   if (p.rows == 32) return launch_rows<DH, F8, 2>(a, p, stream);
-  const dim3 grid(p.row_tiles * a.H * p.pieces);
-  if constexpr (DH == 128) {
-    if (p.rows == kPairRows) hipLaunchKernelGGL((kv_pairs_kernel<F8>), grid, dim3(kPairThreads), 0, stream, a);
-    else hipLaunchKernelGGL((kv_tiles_kernel<DH, F8>), grid, dim3(kThreads), 0, stream, a);
-  } else {
-    hipLaunchKernelGGL((kv_tiles_kernel<DH, F8>), grid, dim3(kThreads), 0, stream, a);
-  }
+  if (a.page % copy_rows(DH) == 0) launch_tiles<DH, F8, true>(a, p, stream);
+  else launch_tiles<DH, F8, false>(a, p, stream);
   if (p.pieces > 1) {
     const long long threads = (long long)a.s.n_tok * a.Hq * (DH / 4);
     hipLaunchKernelGGL((kv_join_kernel<DH>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
