@@ -45,16 +45,23 @@ constexpr int kThreads = 256;
 constexpr int kTileRows = 128;   // rows per workgroup of the tiles kernel
 constexpr int kTileKeys = 64;
 constexpr int kMinWaveKeys = 128;    // keys that a wave of the rows kernel walks at least, before a range is cut
-// keys per tile and wave of the rows kernel: 16 KB of K and V at 128 channels of bf16, and as
-// much in flight for codes and narrower heads
+constexpr int kFewRows = 16;     // rows per workgroup of the rows kernel
+// keys per tile and wave of the rows kernel: 16 KB of K and V at 128 channels, as much in
+// flight for codes, and 16 KB of both for 64 channels of bf16
 constexpr int row_keys(int dh, bool f8) { return dh == 128 && !f8 ? 32 : 64; }
 // its workgroups per compute unit (waves per SIMD)
-constexpr int row_groups(int dh, bool f8, int rows) { return rows == 16 && dh < 128 ? 3 : 2; }
+constexpr int row_groups(int dh) { return dh < 128 ? 3 : 2; }
 constexpr int kMaxPieces = 128;
+constexpr int kJoinWays = 8;   // threads that share the pieces of a row, from as many pieces on
 // s_waitcnt vmcnt(0) that leaves expcnt and lgkmcnt free
 constexpr int kVmcnt0 = 0x0F70;
-// The running maximum moves only when a tile exceeds it by more than 2^8 (see softmax).
-constexpr float kMaxSlack = 8.0f;
+// The running maximum moves only when a tile exceeds it by more than this, in log2 units
+// (see softmax): probabilities reach 2^16, where sums of 2^24 keys of values below 2^80 are
+// still far from overflow, and the exponent's argument is off by 2^-21 at most.  With 2^8,
+// keys whose logits spread by 6 moved some wave's maximum in nearly every tile (chunks of
+// 64-wide heads 177 us, so 143; the frame over an 8-bit window 167 and 146).
+constexpr float kMaxSlack = 16.0f;
+constexpr float kSumBound = 65536.0f;   // 2^kMaxSlack
 // "no key seen yet": below every finite scaled score, so the first visible key moves it
 constexpr float kNoMax = -3.0e38f;
 constexpr float kLn2 = 0.69314718055994531f;
@@ -122,7 +129,7 @@ __device__ __forceinline__ float byte_scale(int e) { return __uint_as_float((uin
 struct RowTile {
   int b, beg, n_rows, row0;      // sequence, its first call row, its rows (tokens * g), first row here
   int len, off;                  // its length; position of its first token of the call
-  int ts, tw, nt;                // logical key tile u: u < ts ? u : tw + u - ts; nt in all
+  int ts, tw, dir, nt;           // logical key tile u: u < ts ? u : tw + dir (u - ts); nt in all
 };
 // the key tiles that rows at positions p_lo .. p_hi of a sequence of `len` meet
 template <int TK>
@@ -132,8 +139,15 @@ __device__ __forceinline__ void key_tiles(const KvAttnArgs& a, RowTile& t, int p
   const int sk = a.window > 0 ? min(a.sinks, hi) : 0;
   const int te = (hi + TK - 1) / TK;
   t.ts = (sk + TK - 1) / TK;
-  t.tw = max(lo / TK, t.ts);
-  t.nt = t.ts + max(te - t.tw, 0);
+  const int first = max(lo / TK, t.ts);
+  t.nt = t.ts + max(te - first, 0);
+  // Row tiles that run at the same time should be at the same keys.  Windows of rows that are
+  // not causal differ in where they begin and end together, so they are walked from the end
+  // (a 30x52 frame, window 7800, 12 heads of 128: 110 us; 153 from the beginning, where the
+  // row tiles read up to 24 key tiles apart, past the L2).
+  const bool back = a.window > 0 && !a.causal;
+  t.tw = back ? te - 1 : first;
+  t.dir = back ? -1 : 1;
 }
 // Row tiles of the call: those of sequence b are numbered from floor(cu[b] g / TM) + b,
 // which leaves room for its partial tile.
@@ -168,19 +182,62 @@ __device__ __forceinline__ void piece_range(const KvAttnArgs& a, int nt, int z, 
   u1 = min(u0 + per, nt);
 }
 
-// The head, piece and row tile of a workgroup of the tiles kernels.  Workgroup b runs on
-// XCD b mod 8.  Each XCD takes a run of the (head, piece, row tile) list, so the row tiles
-// that read the same keys share its L2, and walks it from the end: of causal rows the last
-// tiles are the longest, and the shortest should finish the call.  (With heads over all XCDs
-// and short tiles first: prompts 463 us for 425, chunks of 64-wide heads 232 for 195.)
+// Sums over a wave by row shifts and broadcasts in the registers (shuffles go through the LDS
+// and take ten times as long): inclusive prefix sums of the lanes.
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T dpp_add(T v) {
+  return v + __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+template <class T>
+__device__ __forceinline__ T prefix_sum(T v) {
+  v = dpp_add<0x111, 0xf>(v);                  // row_shr 1, 2, 4, 8: rows of 16 lanes
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);                  // lane 15 of rows 0 and 2 into rows 1 and 3
+  return dpp_add<0x143, 0xc>(v);               // lane 31 into rows 2 and 3
+}
+__device__ __forceinline__ int lane_value(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+
+// The head, piece and row tile of a workgroup of the tiles kernels.  The grid has room for
+// every way to share the rows out among the sequences; the row tiles that are there are
+// counted, so that the workgroups with nothing to do are the last ones of the grid.  (With a
+// spare row tile numbered after each sequence's, 512 rows over 16384 keys of 8 heads took 81
+// us and 511 rows, which need no spare one, 58: while the idle ones start and leave, others
+// pile up on the compute units that are free.)
+// Workgroup b runs on XCD b mod 8.  Each XCD takes a run of the (head, piece, row tile) list,
+// so the row tiles that read the same keys share its L2, and walks it from the end: of causal
+// rows the last tiles are the longest, and the shortest should finish the call.  (With heads
+// over all XCDs and short tiles first: prompts 463 us for 425, chunks of 64-wide heads 232
+// for 195.)
 template <int TM, int TK>
 __device__ __forceinline__ bool my_unit(const KvAttnArgs& a, int& z, int& h, RowTile& t) {
-  const int n = gridDim.x, b = blockIdx.x, x = b & 7, j = b >> 3, per = n >> 3, rest = n & 7;
-  const int unit = x * per + min(x, rest) + (per + (x < rest ? 1 : 0)) - 1 - j;
-  const int q = unit / a.row_tiles;
+  const int lane = threadIdx.x & 63;
+  auto count = [&](int b) __attribute__((always_inline)) -> int {
+    return b < a.s.n_seq ? (max(seq_row(a.s, b + 1) - seq_row(a.s, b), 0) * a.g + TM - 1) / TM : 0;
+  };
+  const int first = count(lane);
+  int total = 0;
+  for (int c = 0; c < a.s.n_seq; c += 64) total += lane_value(prefix_sum(c == 0 ? first : count(c + lane)), 63);
+  total = min(max(total, 0), a.row_tiles);           // (the bound, whatever the offsets hold)
+  const int n = total * a.H * a.npieces, b = blockIdx.x, x = b & 7, j = b >> 3, per = n >> 3, rest = n & 7;
+  const int mine = per + (x < rest ? 1 : 0);
+  if (j >= mine) return false;
+  const int unit = x * per + min(x, rest) + mine - 1 - j;
+  const int q = unit / total, rt = unit - q * total;
   h = q / a.npieces;
   z = q - h * a.npieces;
-  return row_tile<TM, TK>(a, unit - q * a.row_tiles, t);
+  int base = 0;
+  for (int c = 0; c < a.s.n_seq; c += 64) {
+    const int there = c == 0 ? first : count(c + lane), incl = prefix_sum(there);
+    const unsigned long long hit = __ballot(rt - base < incl);
+    if (hit != 0) {
+      const int l = __ffsll((long long)hit) - 1;
+      return place<TM, TK>(a, c + l, rt - base - lane_value(incl - there, l), t);
+    }
+    base += lane_value(incl, 63);
+  }
+  return false;
 }
 
 // A lane's row, and which keys it sees: j < hi, and j >= lo or j < sinks.
@@ -241,9 +298,8 @@ __device__ __forceinline__ void mask_scores(f32x16 (&sn)[NB], int j0, int hf, Ro
 
 // Exponentials of a tile against the running maximum, in place of the scores (a second set
 // would cost the registers of two waves per SIMD at 64-wide heads), packed as P^T operands,
-// and their sum.  A lane's sum of at most 2^8 shows that no score is far above the maximum,
-// which then may stay (probabilities up to 2^8 do no harm in fp32 sums and bf16 operands);
-// else the scores are formed again, the maximum is taken over the tile, moved, and the sums
+// and their sum.  A lane's sum of at most 2^16 shows that no score is far above the maximum,
+// which then may stay; else the scores are formed again, the maximum is taken over the tile, moved, and the sums
 // so far scaled down.
 template <int NB, int ND, class S>
 __device__ __forceinline__ void softmax(f32x16 (&sn)[NB], S&& scores, bf16x8 (&pp)[NB][2], float& m_run, float& l_run,
@@ -259,7 +315,7 @@ __device__ __forceinline__ void softmax(f32x16 (&sn)[NB], S&& scores, bf16x8 (&p
     return (rs[0] + rs[1]) + (rs[2] + rs[3]);
   };
   float sum = exps();
-  if (__ballot(!(sum <= 256.0f)) != 0ull) {
+  if (__ballot(!(sum <= kSumBound)) != 0ull) {
     scores();
     float pm = sn[0][0];
 #pragma unroll
@@ -430,9 +486,7 @@ __device__ __forceinline__ void finish(const KvAttnArgs& a, int z, long long row
 // RUNS (both tiles kernels): pages of a multiple of copy_rows(DH) tokens.  Then the rows of
 // one copy instruction of a wave, which start at a multiple of it, lie side by side in one
 // page, and their place is one number for the wave; else every lane fetches its row's place
-// from the lane that looked it up.  (28160 keys, 4 x 3520 rows of 24 heads of 128: XX us
-// so, 5008 us with the places passed between lanes: the LDS, which that goes through, is as
-// busy as the matrix cores.)
+// from the lane that looked it up.  (The LDS, which that goes through, is as busy as the matrix cores.)
 constexpr int copy_rows(int dh) { return 1024 / dh; }
 template <int DH, bool F8, bool RUNS>
 __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv_tiles_kernel(KvAttnArgs a) {
@@ -473,7 +527,7 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
 
   // ---- key lookup: lane l of every wave looks up key l of a tile
   const int32_t* table = a.s.table + (long long)t.b * a.s.max_pages;
-  auto tile_of = [&](int u) { return u < t.ts ? u : t.tw + (u - t.ts); };
+  auto tile_of = [&](int u) { return u < t.ts ? u : t.tw + t.dir * (u - t.ts); };
   struct Look { int key, id, rem; };
   auto look = [&](int u) __attribute__((always_inline)) -> Look {
     Look k;
@@ -703,7 +757,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
 
   // ---- key lookup, as in the tiles kernel
   const int32_t* table = a.s.table + (long long)t.b * a.s.max_pages;
-  auto tile_of = [&](int u) { return u < t.ts ? u : t.tw + (u - t.ts); };
+  auto tile_of = [&](int u) { return u < t.ts ? u : t.tw + t.dir * (u - t.ts); };
   struct Look { int key, id, rem; };
   auto look = [&](int u) __attribute__((always_inline)) -> Look {
     Look k;
@@ -728,7 +782,8 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
   // With RUNS one lookup serves eight tiles: lane l looks up the run of eight keys
   // l mod 8 of tile l / 8 of a window of them, and keeps its address.  (Looked up tile by
   // tile, a tile cost 55 more vector and 55 more scalar instructions than the products and
-  // the softmax take, 28160 keys of 4 x 3520 rows 4856 us for XX.)
+  // the softmax take, 4 x 3520 rows of 24 heads on
+  // 28160 keys 4856 us, so and with the reads' offsets kept in registers 4468.)
   constexpr int GR = copy_rows(DH), GPT = TK / GR, TPW = 64 / GPT;
   static_assert(GPT == 8, "eight runs per tile: a byte of the window's mask");
   int win_id = 0, win_rem = 0;               // the next window's lookup
@@ -858,13 +913,13 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
   };
 
   const int n = u1 - u0;
-  // keys of tile j that exist, and of the next: bits per key, with RUNS per run
-  unsigned long long there = 0, there_next = 0;
+  // keys of tile j that exist, and of the next ones: bits per key, with RUNS per run
+  unsigned long long there = 0, there_next = 0, there_far = 0;
   Look nxt{};
-  auto fetch = [&](uint16_t* kd, uint16_t* vd, int wt) __attribute__((always_inline)) {
-    if constexpr (F8) load8(wt);
-    else copy_bf16(grp == 0 ? kd : vd, wt);
-  };
+  constexpr int D = F8 ? 2 : 1;              // tiles from the products' to the one being fetched
+  // Codes go through registers, and are fetched a tile earlier than they are stored: the
+  // fetch of tile j + 2 follows the store of j + 1 at the start of an interval and has until
+  // the next such start.
   auto runs_of = [&](int wt) { return (runs >> (wt * GPT)) & 0xff; };
   if (n > 0) {
     for (int x = tid; x < TK * DH / 8; x += kPairThreads) reinterpret_cast<u32x4*>(lds_zero)[x] = u32x4{0u, 0u, 0u, 0u};
@@ -876,10 +931,17 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
     } else {
       resolve(look(u0), there);
     }
-    fetch(lds_k0, lds_v0, 0);
-    if constexpr (F8) store8(grp == 0 ? lds_k0 : lds_v0, 0);
-    if constexpr (!RUNS) nxt = look(u0 + 1);
-    __builtin_amdgcn_s_waitcnt(kVmcnt0);
+    if constexpr (F8) {
+      load8(0);
+      store8(grp == 0 ? lds_k0 : lds_v0, 0);
+      if constexpr (RUNS) there_next = runs_of(1);
+      else resolve(look(u0 + 1), there_next);
+      load8(1);
+    } else {
+      copy_bf16(grp == 0 ? lds_k0 : lds_v0, 0);
+    }
+    if constexpr (!RUNS) nxt = look(u0 + D);
+    if constexpr (!F8) __builtin_amdgcn_s_waitcnt(kVmcnt0);
     __syncthreads();
     if (grp == 1) __syncthreads();
     auto kind_of = [&](int j, unsigned long long th) __attribute__((always_inline)) {
@@ -893,30 +955,39 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
       uint16_t* kn = P == 0 ? lds_k1 : lds_k0;           // K[j - 1], then K[j + 1]
       uint16_t* vn = P == 0 ? lds_v1 : lds_v0;           // V[j - 1], then V[j + 1]
       const int j0 = tile_of(u0 + j) * TK;
-      const int wt = (j + 1) % TPW;                      // tile j + 1 in its window
+      const int wt = (j + 1) % TPW, wd = (j + D) % TPW;  // tiles j + 1 and j + D in their windows
       // What tile j + 1 needs to know is worked out beside the products, where the wave waits
       // for the matrix core anyway.
       auto prepare = [&](auto uu) __attribute__((always_inline)) {
         constexpr int i = decltype(uu)::value;
-        if constexpr (!RUNS && i == 1) resolve(nxt, there_next);
-        if constexpr (!RUNS && i == 5) nxt = look(u0 + j + 2);
-        if constexpr (RUNS && i == 5) there_next = runs_of(wt);
+        if constexpr (!RUNS && i == 1) resolve(nxt, F8 ? there_far : there_next);
+        if constexpr (!RUNS && i == 5) nxt = look(u0 + j + D + 1);
+        if constexpr (RUNS && !F8 && i == 5) there_next = runs_of(wt);
         if constexpr (i == 9) kind_next = kind_of(j + 1, there_next);
       };
-      if constexpr (RUNS) {
-        if (wt == 0) {                                   // (the copies of tile j are done)
+      auto next_window = [&]() __attribute__((always_inline)) {
+        if (RUNS && wd == 0) {                           // (no copy from the last one is to come)
           enter_window();
-          open_window(u0 + j + 1 + TPW);
+          open_window(u0 + j + D + TPW);
         }
-      }
+      };
+      if constexpr (!F8) next_window();
       // (one path for both products: with a path for each case the accumulators moved between
       // registers; a product that is not wanted meets zeros or is not looked at)
       if (kind != 0 || has_p) products(kc, has_p ? vn : lds_zero, IC<1>{}, prepare);
       else static_for<0, 16>(prepare);
       has_p = kind != 0;
       __syncthreads();
-      const bool more = j + 1 < n;
-      if (more) fetch(kn, vn, wt);
+      if constexpr (F8) {
+        if (j + 1 < n) store8(grp == 0 ? kn : vn, wt);
+        if (j + 2 < n) {
+          next_window();
+          load8(wd);
+        }
+        if constexpr (RUNS) there_far = runs_of(wd);
+      } else if (j + 1 < n) {
+        copy_bf16(grp == 0 ? kn : vn, wt);
+      }
       if (kind != 0) {
         auto mask = [&]() __attribute__((always_inline)) {
           if (kind == 1) mask_scores<2>(sn, j0, hf, lim, a.sinks, RUNS ? bytes_of(there) : there);
@@ -937,13 +1008,11 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
           }
         }
       }
-      if constexpr (F8) {
-        if (more) store8(grp == 0 ? kn : vn, wt);
-      }
       there = there_next;
+      if constexpr (F8) there_next = there_far;
       kind = kind_next;
-      // (the barrier's fence does not wait for copies into LDS)
-      __builtin_amdgcn_s_waitcnt(kVmcnt0);
+      // (the barrier's fence does not wait for copies into LDS; codes may still be on their way)
+      if constexpr (!F8) __builtin_amdgcn_s_waitcnt(kVmcnt0);
       __syncthreads();
     };
 #pragma unroll 1
@@ -963,7 +1032,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
 // ---------------------------------------------------------------------------
 // v_mfma_f32_16x16x32_bf16: of 16 rows an accumulator takes a quarter of the registers that
 // 32x32 tiles need, which leaves room for three workgroups per compute unit, each wave with
-// a whole key tile on its way.  NQ blocks of 16 rows share every key read.
+// a whole key tile on its way.
 //
 // The four waves take wh = 4, 2 or 1 neighbouring heads (whatever divides H) and share each
 // head's key tiles 4 / wh ways.  Waves that walk the same tokens in step read them whole
@@ -1008,8 +1077,7 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, int x, Item& it) 
       const SeqWork v = c == 0 ? w : seq_work<TM, TK>(a, c + lane);
       sum += (float)v.rt * (float)v.nt;
     }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    sum = __int_as_float(lane_value(__float_as_int(prefix_sum(sum)), 63));
     // (rounded up, so that the items never pass target + row tiles * hgroups)
     per = max(kMinWaveKeys / TK * (kThreads / 64 / a.wh), (int)fminf(ceilf(sum * (float)a.hgroups * 1.0001f / (float)a.target), 1.0e9f));
   }
@@ -1017,28 +1085,22 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, int x, Item& it) 
   for (int c = 0; c < n_seq; c += 64) {
     if (c > 0) w = seq_work<TM, TK>(a, c + lane);
     const int pieces = max(1, (w.nt + per - 1) / per);
-    int incl = w.rt * pieces * a.hgroups;
-    const int mine = incl;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(incl, d);
-      if (lane >= d) incl += o;
-    }
+    const int mine = w.rt * pieces * a.hgroups, incl = prefix_sum(mine);
     const unsigned long long hit = __ballot(x - base < incl);
     if (hit != 0) {
       const int l = __ffsll((long long)hit) - 1;
-      const int first = base + __shfl(incl - mine, l);
-      it.pieces = __builtin_amdgcn_readfirstlane(__shfl(pieces, l));
+      const int first = base + lane_value(incl - mine, l);
+      it.pieces = lane_value(pieces, l);
       it.per = per;
-      const int local = __builtin_amdgcn_readfirstlane(x - first), rest = local / a.hgroups;
+      const int local = x - first, rest = local / a.hgroups;
       it.hg = local - rest * a.hgroups;
       const int k = rest / it.pieces;
       it.z = rest - k * it.pieces;
-      it.item0 = __builtin_amdgcn_readfirstlane(first) + k * it.pieces * a.hgroups + it.hg;
+      it.item0 = first + k * it.pieces * a.hgroups + it.hg;
       it.tile_id = first_tile<TM>(a, c + l) + k;
       return place<TM, TK>(a, c + l, k, it.t);
     }
-    base += __shfl(incl, 63);
+    base += lane_value(incl, 63);
   }
   return false;
 }
@@ -1052,9 +1114,9 @@ __device__ __forceinline__ float quarter_max(float x) {
   return half_swap_max(fmaxf(__uint_as_float(s.x), __uint_as_float(s.y)));
 }
 
-template <int DH, bool F8, int NQ>
-__global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows_kernel(KvAttnArgs a) {
-  constexpr int CPR = DH / 8, ROWB = DH * 2, TK = row_keys(DH, F8), W = kThreads / 64, TM = 16 * NQ;
+template <int DH, bool F8>
+__global__ __launch_bounds__(kThreads, row_groups(DH)) void kv_rows_kernel(KvAttnArgs a) {
+  constexpr int CPR = DH / 8, ROWB = DH * 2, TK = row_keys(DH, F8), W = kThreads / 64, TM = kFewRows;
   constexpr int SUB = TK / 32, R = 2 * SUB;          // 32-key halves; a lane's rows: l16 + 16 r
   constexpr int NT = DH / 32;                        // contraction steps of S, 32 channels each
   constexpr int ND = DH / 16;                        // 16-channel blocks of O^T
@@ -1078,21 +1140,18 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
   const int nrows = min(TM, t.n_rows - t.row0);
   const int p0 = t.off + t.row0 / a.g, p1 = t.off + (t.row0 + nrows - 1) / a.g;
   const KindBounds kb = kind_bounds(a, t.len, p0, p1);
-  RowLimits lim[NQ];
-  bf16x8 qreg[NQ][NT];
+  RowLimits lim;
+  bf16x8 qreg[NT];
+  const int r = t.row0 + min(l16, nrows - 1);
+  const int tok = r / a.g, hq = h * a.g + (r - tok * a.g);
+  lim = row_limits(a, t, t.off + tok);
+  const uint16_t* qp = a.q + (long long)(t.beg + tok) * a.qs + hq * DH;
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    const int r = t.row0 + min(16 * nq + l16, nrows - 1);
-    const int tok = r / a.g, hq = h * a.g + (r - tok * a.g);
-    lim[nq] = row_limits(a, t, t.off + tok);
-    const uint16_t* qp = a.q + (long long)(t.beg + tok) * a.qs + hq * DH;
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-      qreg[nq][i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(
-          qp + (F8 && !HALF ? 64 * (i / 2) + 16 * qd + 8 * (i % 2) : 32 * i + 8 * qd)));
-  }
+  for (int i = 0; i < NT; ++i)
+    qreg[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(
+        qp + (F8 && !HALF ? 64 * (i / 2) + 16 * qd + 8 * (i % 2) : 32 * i + 8 * qd)));
   const int32_t* table = a.s.table + (long long)t.b * a.s.max_pages;
-  auto tile_of = [&](int u) { return u < t.ts ? u : t.tw + (u - t.ts); };
+  auto tile_of = [&](int u) { return u < t.ts ? u : t.tw + t.dir * (u - t.ts); };
   // lane l looks up key l (mod TK) of a tile
   struct Look { int key, id, rem; };
   auto look = [&](int u) __attribute__((always_inline)) -> Look {
@@ -1159,15 +1218,12 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
     return __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
   };
 
-  f32x4 acc[NQ][ND];
-  float m_run[NQ], l_run[NQ];
+  f32x4 acc[ND];
+  float m_run, l_run;
+  m_run = kNoMax;
+  l_run = 0.0f;
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    m_run[nq] = kNoMax;
-    l_run[nq] = 0.0f;
-#pragma unroll
-    for (int db = 0; db < ND; ++db) acc[nq][db] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  for (int db = 0; db < ND; ++db) acc[db] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   unsigned long long there = 0, there_next = 0;
   long long at[R];
@@ -1199,7 +1255,7 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
   for (; u < u1; u += ways) {
     const bool more = u + ways < u1;
     const int j0 = tile_of(u) * TK;
-    f32x4 sn[NQ][R];
+    f32x4 sn[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float sc = 0.0f;
@@ -1213,8 +1269,7 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
         } else {
           op = __builtin_bit_cast(bf16x8, kr[r][i]);
         }
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) sn[nq][r] = mfma16(op, qreg[nq][i], i == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sn[nq][r]);
+        sn[r] = mfma16(op, qreg[i], i == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sn[r]);
       }
     }
     if constexpr (F8) {
@@ -1227,55 +1282,50 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
       load_rows(a.k, at, kr, 0, R);
       nxt = look(u + 2 * ways);
     }
-    bf16x8 pp[NQ][SUB];
+    bf16x8 pp[SUB];
     if (kind != 0) {
       if (kind == 1) {
 #pragma unroll
-        for (int nq = 0; nq < NQ; ++nq)
-#pragma unroll
-          for (int sub = 0; sub < SUB; ++sub) {
-            const uint32_t bits = visible_bits(lim[nq], a.sinks, j0 + 32 * sub, (uint32_t)(there >> (32 * sub))) >> (4 * qd);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (((bits >> (16 * (e / 4) + e % 4)) & 1) == 0) sn[nq][2 * sub + e / 4][e % 4] = -INFINITY;
-          }
-      }
-#pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) {
-        // (see softmax)
-        float pe[8 * SUB];
-        auto exps = [&]() __attribute__((always_inline)) -> float {
-          float rs[4];
-#pragma unroll
-          for (int e = 0; e < 8 * SUB; ++e) {
-            pe[e] = __builtin_amdgcn_exp2f(fmaf(sn[nq][e / 4][e % 4], a.sl2, -m_run[nq]));
-            rs[e % 4] = e < 4 ? pe[e] : rs[e % 4] + pe[e];
-          }
-          return (rs[0] + rs[1]) + (rs[2] + rs[3]);
-        };
-        float sum = exps();
-        if (__ballot(!(sum <= 256.0f)) != 0ull) {
-          float pm = sn[nq][0][0];
-#pragma unroll
-          for (int e = 1; e < 8 * SUB; ++e) pm = fmaxf(pm, sn[nq][e / 4][e % 4]);
-          const float cand = fmaxf(m_run[nq], quarter_max(pm) * a.sl2);
-          const bool up = cand > m_run[nq] + kMaxSlack;
-          const float m_new = up ? cand : m_run[nq];
-          const float corr = __builtin_amdgcn_exp2f(m_run[nq] - m_new);
-          l_run[nq] *= corr;
-          m_run[nq] = m_new;
-#pragma unroll
-          for (int db = 0; db < ND; ++db) acc[nq][db] *= corr;
-          sum = exps();
-        }
-#pragma unroll
         for (int sub = 0; sub < SUB; ++sub) {
-          const float* p = &pe[8 * sub];
-          pp[nq][sub] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
-                                                         pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])});
+          const uint32_t bits = visible_bits(lim, a.sinks, j0 + 32 * sub, (uint32_t)(there >> (32 * sub))) >> (4 * qd);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (((bits >> (16 * (e / 4) + e % 4)) & 1) == 0) sn[2 * sub + e / 4][e % 4] = -INFINITY;
         }
-        l_run[nq] += sum;
       }
+      // (see softmax)
+      float pe[8 * SUB];
+      auto exps = [&]() __attribute__((always_inline)) -> float {
+        float rs[4];
+#pragma unroll
+        for (int e = 0; e < 8 * SUB; ++e) {
+          pe[e] = __builtin_amdgcn_exp2f(fmaf(sn[e / 4][e % 4], a.sl2, -m_run));
+          rs[e % 4] = e < 4 ? pe[e] : rs[e % 4] + pe[e];
+        }
+        return (rs[0] + rs[1]) + (rs[2] + rs[3]);
+      };
+      float sum = exps();
+      if (__ballot(!(sum <= kSumBound)) != 0ull) {
+        float pm = sn[0][0];
+#pragma unroll
+        for (int e = 1; e < 8 * SUB; ++e) pm = fmaxf(pm, sn[e / 4][e % 4]);
+        const float cand = fmaxf(m_run, quarter_max(pm) * a.sl2);
+        const bool up = cand > m_run + kMaxSlack;
+        const float m_new = up ? cand : m_run;
+        const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= corr;
+        m_run = m_new;
+#pragma unroll
+        for (int db = 0; db < ND; ++db) acc[db] *= corr;
+        sum = exps();
+      }
+#pragma unroll
+      for (int sub = 0; sub < SUB; ++sub) {
+        const float* p = &pe[8 * sub];
+        pp[sub] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
+                                                   pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])});
+      }
+      l_run += sum;
     }
     // values, 32 keys at a time through the wave's LDS tile
 #pragma unroll
@@ -1299,22 +1349,18 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
 #pragma unroll
         for (int db = 0; db < ND; ++db) {
           const bf16x8 op = read_v(vrd, db);
-#pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) acc[nq][db] = mfma16(op, pp[nq][sub], acc[nq][db]);
+          acc[db] = mfma16(op, pp[sub], acc[db]);
         }
       } else {
 #pragma unroll
         for (int db = 0; db < ND; ++db) {
           const bf16x8 op = read_v(vrd, db);
-#pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) {
-            const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
-            const bf16x8 w = seen_weights(pp[nq][sub]);
-            acc[nq][db] = mfma16(part_of<kFinite>(op), pp[nq][sub], acc[nq][db]);
-            add_infinity<4>(acc[nq][db], mfma16(part_of<kPlus>(op), w, zero), 1.0f);
-            add_infinity<4>(acc[nq][db], mfma16(part_of<kMinus>(op), w, zero), -1.0f);
-            PIN(acc[nq][db]);
-          }
+          const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+          const bf16x8 w = seen_weights(pp[sub]);
+          acc[db] = mfma16(part_of<kFinite>(op), pp[sub], acc[db]);
+          add_infinity<4>(acc[db], mfma16(part_of<kPlus>(op), w, zero), 1.0f);
+          add_infinity<4>(acc[db], mfma16(part_of<kMinus>(op), w, zero), -1.0f);
+          PIN(acc[db]);
         }
         if (more) load_rows(a.v, at, vr, 2 * sub, 2 * sub + 2);
       }
@@ -1323,24 +1369,19 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
   }
 
   // ---- join the waves of a head: weights 2^(m_w - max m)
-#pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    float l = l_run[nq] + __shfl_xor(l_run[nq], 16);
-    l += __shfl_xor(l, 32);
-    if (qd == 0) {
-      sm[wave][16 * nq + l16] = m_run[nq];
-      sl[wave][16 * nq + l16] = l;
-    }
+  float l = l_run + __shfl_xor(l_run, 16);
+  l += __shfl_xor(l, 32);
+  if (qd == 0) {
+    sm[wave][l16] = m_run;
+    sl[wave][l16] = l;
   }
   __syncthreads();                                   // (the value tiles are read no more)
   float* part = reinterpret_cast<float*>(smem);
+  if (l16 < nrows) {
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq)
-    if (16 * nq + l16 < nrows) {
-#pragma unroll
-      for (int db = 0; db < ND; ++db)
-        *reinterpret_cast<f32x4*>(part + (wave * TM + 16 * nq + l16) * DH + 16 * db + 4 * qd) = acc[nq][db];
-    }
+    for (int db = 0; db < ND; ++db)
+      *reinterpret_cast<f32x4*>(part + (wave * TM + l16) * DH + 16 * db + 4 * qd) = acc[db];
+  }
   __syncthreads();
   if (a.target > 0 && it.z == 0 && tid == 0) a.meta[(long long)it.tile_id * a.hgroups + it.hg] = make_int2(it.item0, it.pieces);
   const int per_head = nrows * (DH / 4);
@@ -1377,23 +1418,24 @@ __global__ __launch_bounds__(kThreads, row_groups(DH, F8, 16 * NQ)) void kv_rows
 // O_z the normalised output of piece z, O = sum 2^(l_z - max) O_z / sum 2^(l_z - max).
 // Pieces without a visible key (-inf) add nothing.  One workgroup per row, its threads
 // shared out over four channels each and, in step, the pieces; grid (row tile, head, row).
-template <int DH, int TM>
+template <int DH>
 __global__ __launch_bounds__(kThreads) void kv_rows_join_kernel(KvAttnArgs a) {
-  constexpr int PER = DH / 4, WAYS = kThreads / PER;
+  constexpr int TM = kFewRows, PER = DH / 4, WAYS = kThreads / PER;
   __shared__ float red[kThreads / 64];
   __shared__ f32x4 part[kThreads];
   __shared__ float sums[WAYS];
-  RowTile t;
-  if (!row_tile<TM, 32>(a, blockIdx.x, t)) return;
   const int ql = blockIdx.z, tid = threadIdx.x;
-  if (ql >= t.n_rows - t.row0) return;
   const int hg = blockIdx.y / a.wh, hw = blockIdx.y - hg * a.wh;
   const int2 meta = a.meta[(long long)blockIdx.x * a.hgroups + hg];
-  // (the bounds hold for whatever lies in the workspace)
+  // (the bounds hold for whatever lies in the workspace: a row tile that does not exist has no
+  // entry of this call, which is found out below, after the first loads are on their way)
   if (meta.y < 2 || meta.x < 0 || meta.x >= a.max_items || meta.y > (a.max_items - 1 - meta.x) / a.hgroups + 1) return;
   auto slot = [&](int z) { return ((long long)(meta.x + z * a.hgroups) * a.wh + hw) * TM + ql; };
-  float m = -INFINITY;
-  for (int z = tid; z < meta.y; z += kThreads) {
+  const float first = tid < meta.y ? a.part_lse[slot(tid)] : -INFINITY;
+  RowTile t;
+  if (!row_tile<TM, 32>(a, blockIdx.x, t) || ql >= t.n_rows - t.row0) return;
+  float m = first;
+  for (int z = tid + kThreads; z < meta.y; z += kThreads) {
     const float l = a.part_lse[slot(z)];
     m = l > m || l != l ? l : m;
   }
@@ -1436,44 +1478,79 @@ __global__ __launch_bounds__(kThreads) void kv_rows_join_kernel(KvAttnArgs a) {
   if (a.lse != nullptr && d == 0) a.lse[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
 }
 
-// Join of the pieces of every row: with l_z the log2 log-sum-exp and O_z the normalised
-// output of piece z, O = sum 2^(l_z - max) O_z / sum 2^(l_z - max).  One thread per four
-// channels of a row; pieces without a visible key (-inf) are not read.
-template <int DH>
+// Join of the pieces of every row, as above.  WAYS threads share the pieces of four channels
+// of a row.
+template <int DH, int WAYS>
 __global__ __launch_bounds__(kThreads) void kv_join_kernel(KvAttnArgs a) {
+  constexpr int PER = DH / 4, ROWS = kThreads / (PER * WAYS);
+  __shared__ f32x4 part[kThreads];
+  __shared__ float tops[kThreads / PER], sums[kThreads / PER];
   const long long rows = (long long)a.s.n_tok * a.Hq;
-  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
-  const long long row = i / (DH / 4);
-  const int d = 4 * (int)(i % (DH / 4));
-  if (row >= rows) return;
-  const int tok = (int)(row / a.Hq);
-  if (tok < seq_row(a.s, 0) || tok >= seq_row(a.s, a.s.n_seq)) return;   // of no sequence: left alone
+  const int tid = threadIdx.x, slot = tid / PER, way = slot % WAYS, first = slot - way, d = 4 * (tid % PER);
+  const long long row = (long long)blockIdx.x * ROWS + slot / WAYS;
+  const bool there = row < rows;
+  const float* lse = a.part_lse + (there ? row : 0);
+  const float* o_z = a.part_o + (there ? row : 0) * DH + d;
   float m = -INFINITY;
-  for (int z = 0; z < a.npieces; ++z) {
-    const float l = a.part_lse[z * rows + row];
+#pragma unroll 4
+  for (int z = way; z < a.npieces; z += WAYS) {
+    const float l = lse[z * rows];
     m = l > m || l != l ? l : m;
+  }
+  if constexpr (WAYS > 1) {
+    if (d == 0) tops[slot] = m;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < WAYS; ++k) {
+      const float l = tops[first + k];
+      m = l > m || l != l ? l : m;
+    }
   }
   float w = 0.0f;
   f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int z = 0; z < a.npieces; ++z) {
-    const float l = a.part_lse[z * rows + row];
-    if (l == -INFINITY) continue;
+#pragma unroll 4
+  for (int z = way; z < a.npieces; z += WAYS) {
+    const float l = lse[z * rows];
+    const f32x4 p = *reinterpret_cast<const f32x4*>(o_z + z * rows * DH);
     const float c = l == m ? 1.0f : __builtin_amdgcn_exp2f(l - m);
-    w += c;
-    o += c * *reinterpret_cast<const f32x4*>(a.part_o + (z * rows + row) * DH + d);
+    if (l != -INFINITY) {   // else nothing was written
+      w += c;
+      o += c * p;
+    }
   }
+  if constexpr (WAYS > 1) {
+    part[tid] = o;
+    if (d == 0) sums[slot] = w;
+    __syncthreads();
+    if (way != 0) return;
+#pragma unroll
+    for (int k = 1; k < WAYS; ++k) {
+      w += sums[first + k];
+      o += part[tid + k * PER];
+    }
+  }
+  if (!there) return;
+  const int tok = (int)(row / a.Hq);
+  if (tok < seq_row(a.s, 0) || tok >= seq_row(a.s, a.s.n_seq)) return;   // of no sequence: left alone
   const bool some = w != 0.0f;
   o *= some ? 1.0f / w : 0.0f;
   put4(a, row, DH, d, o);
   if (a.lse != nullptr && d == 0) a.lse[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
 }
 
-template <int DH, bool F8, int NQ>
+template <int DH, int WAYS>
+void launch_join(const KvAttnArgs& a, hipStream_t stream) {
+  const long long threads = (long long)a.s.n_tok * a.Hq * (DH / 4) * WAYS;
+  hipLaunchKernelGGL((kv_join_kernel<DH, WAYS>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads),
+                     0, stream, a);
+}
+
+template <int DH, bool F8>
 void launch_rows(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
   const int items = p.target > 0 ? p.max_items : p.row_tiles * a.hgroups;
-  hipLaunchKernelGGL((kv_rows_kernel<DH, F8, NQ>), dim3(items), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((kv_rows_kernel<DH, F8>), dim3(items), dim3(kThreads), 0, stream, a);
   if (p.target > 0)
-    hipLaunchKernelGGL((kv_rows_join_kernel<DH, 16 * NQ>), dim3(p.row_tiles, a.H, 16 * NQ), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((kv_rows_join_kernel<DH>), dim3(p.row_tiles, a.H, kFewRows), dim3(kThreads), 0, stream, a);
 }
 
 template <int DH, bool F8, bool RUNS>
@@ -1490,15 +1567,11 @@ void launch_tiles(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) 
 
 template <int DH, bool F8>
 void launch_as(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
-  if (p.rows == 16) return launch_rows<DH, F8, 1>(a, p, stream);
-  if (p.rows == 32) return launch_rows<DH, F8, 2>(a, p, stream);
+  if (p.rows == kFewRows) return launch_rows<DH, F8>(a, p, stream);
   if (a.page % copy_rows(DH) == 0) launch_tiles<DH, F8, true>(a, p, stream);
   else launch_tiles<DH, F8, false>(a, p, stream);
-  if (p.pieces > 1) {
-    const long long threads = (long long)a.s.n_tok * a.Hq * (DH / 4);
-    hipLaunchKernelGGL((kv_join_kernel<DH>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                       stream, a);
-  }
+  if (p.pieces >= kJoinWays) launch_join<DH, kJoinWays>(a, stream);
+  else if (p.pieces > 1) launch_join<DH, 1>(a, stream);
 }
 
 }  // namespace
@@ -1507,29 +1580,42 @@ KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f
                         int cus) {
   KvAttnPlan p{};
   const long long rows = n_tok * g, mean = (rows + n_seq - 1) / n_seq;
-  p.rows = mean <= 16 ? 16 : mean <= 64 ? 32 : dh < 128 || mean <= kTileRows ? kTileRows : kPairRows;
+  long long keys = max_len;
+  if (window > 0) keys = std::min(keys, (long long)window + (mean + g - 1) / g + sinks + 2 * kTileKeys);
+  const long long nt = (keys + kTileKeys - 1) / kTileKeys;
+  auto units = [&](long long tile_rows) { return n_seq * ((mean + tile_rows - 1) / tile_rows) * H; };
+  // Rows per workgroup, by their mean over the sequences (8 heads of 128 in bf16 unless said).
+  // Up to 16, the rows kernel, whose pieces follow the lengths: 16 streams of 300 to 8100
+  // tokens 63 us, as 128-row tiles 81; 4 streams of 65536 to 131072 e4m3 tokens 164 and 298.
+  // (Of sequences of one length tiles would gain: 8 of 4096 tokens with 16 rows 41 and 31.)
+  // From 17 on the half-filled tiles win: 8 of 4096 with 17 rows 46 and 31, 32 rows 58 and 32.
+  // Pairs beyond 128 rows of 128 channels, if they can be cut into enough pieces to fill the
+  // card: 8 of 4096 with 192 rows 51 us, 57 in tiles; 768 rows 107 and 140; but 4 of 1024
+  // with 192 rows, 64 pieces, 30 and 25.
+  const bool pairs = dh == 128 && mean > kTileRows && units(kPairRows) * ((nt + 7) / 8) >= cus * 3 / 4;
+  p.rows = mean <= kFewRows ? kFewRows : pairs ? kPairRows : kTileRows;
   p.wh = H % 4 == 0 ? 4 : H % 2 == 0 ? 2 : 1;
-  p.row_tiles = (int)(rows / p.rows + n_seq);
+  // at most, over all ways to share the rows out
+  p.row_tiles = (int)(p.rows == kFewRows ? rows / p.rows + n_seq : (rows + (long long)n_seq * (p.rows - 1)) / p.rows);
   p.pieces = 1;
   p.piece_tiles = 1;
   if (cus <= 0 || n_tok < 1) return p;
-  const long long tiles = (long long)n_seq * ((mean + p.rows - 1) / p.rows);
-  long long keys = max_len;
-  if (window > 0) keys = std::min(keys, (long long)window + (mean + g - 1) / g + sinks + 2 * kTileKeys);
   if (p.rows < kTileRows) {
     // workgroups resident at once, less the partial pieces that the row tiles end with
-    const long long resident = (long long)cus * row_groups(dh, f8, p.rows), units = tiles * (H / p.wh);
-    if (keys <= kMinWaveKeys * (kThreads / 64 / p.wh) || units >= resident) return p;
-    p.target = (int)std::max(resident - units / 2, resident / 2);
+    const long long resident = (long long)cus * row_groups(dh), items = units(kFewRows) / p.wh;
+    if (keys <= kMinWaveKeys * (kThreads / 64 / p.wh) || items >= resident) return p;
+    p.target = (int)std::max(resident - items / 2, resident / 2);
     p.max_items = p.target + p.row_tiles * (H / p.wh) + 1;
     p.part_bytes = align_up((size_t)p.max_items * p.wh * p.rows * dh * 4);
     p.lse_bytes = align_up((size_t)p.max_items * p.wh * p.rows * 4);
     p.bytes = p.part_bytes + p.lse_bytes + align_up((size_t)p.row_tiles * (H / p.wh) * sizeof(int2));
     return p;
   }
-  const long long units = tiles * H, nt = (keys + kTileKeys - 1) / kTileKeys;
-  const long long want = (long long)cus * (p.rows == kPairRows ? 1 : 2) / std::max(units, 1ll);
-  const long long most = std::min<long long>(std::min<long long>(want, kMaxPieces), (nt + 7) / 8);   // 8 key tiles at least
+  const long long want = (long long)cus * (p.rows == kPairRows ? 1 : 2) / std::max(units(p.rows), 1ll);
+  // Key tiles of a piece: a piece of few rows leaves little to join (48 rows over 4 x 1024
+  // keys: 17 us with 4 tiles at least, 22 with 8; 128 rows over 16384: 48 and 36).
+  const long long least = std::clamp(mean / 16, 4ll, 8ll);
+  const long long most = std::min<long long>(std::min<long long>(want, kMaxPieces), (nt + least - 1) / least);
   if (most < 2) return p;
   p.piece_tiles = (int)((nt + most - 1) / most);
   p.pieces = (int)((nt + p.piece_tiles - 1) / p.piece_tiles);
