@@ -532,7 +532,9 @@ cast_status_t cast_rope(const void* x, int dtype, int n, int H, int dh, long lon
 /*
  * A paged cache.  dtype 1: bf16 values.  dtype 2: e4m3 codes (OCP, 1-4-3 bits) with one
  * exponent byte per (page, head), value = code * 2^(byte - 127).  The scales are powers
- * of two, so every value of an 8-bit cache is a bf16 number exactly.
+ * of two, so every value of an 8-bit cache is a bf16 number exactly.  (cast_kv_append
+ * writes bytes 10 .. 247.  Byte 247 belongs to values next to the largest bf16 number,
+ * and those that round up from there are infinite.)
  */
 typedef struct {
   void* k;                /* device [pages, page, H, dh] bf16 or uint8 codes            */
@@ -581,9 +583,10 @@ typedef struct {
  * that page, nothing outside it); rows of a page behind the last token are not touched.
  * Tensors must not overlap the cache.  n_seq >= 1, n_tok >= 0 (0: nothing is enqueued);
  * 16-byte aligned tensors (int32 ones 4-byte); H <= 4096, page < 2^24,
- * pages * page < 2^31, page * H * H < 2^40; n_seq <= 2^20, n_tok < 2^30, max_pages < 2^24,
+ * pages * page < 2^31, page * H * H < 2^40; n_seq <= 2^20, n_tok <= 2^25, max_pages < 2^24,
  * max_pages * page < 2^30, max_pages * page * page and n_tok * page < 2^40, n_tok < 2^24 page
- * (the same limits hold for every call on a cache).
+ * (the same limits hold for every call on a cache); an 8-bit cache takes fewer than 2^24
+ * (page, head) pieces of K and V in a call.
  * Errors: CAST_ERR_NULL, CAST_ERR_SHAPE, CAST_ERR_UNSUPPORTED (dh; sizes past the limits).
  */
 cast_status_t cast_kv_append(const cast_kv_cache_t* cache, const cast_kv_seqs_t* seqs,
@@ -621,7 +624,7 @@ size_t cast_kv_attn_workspace_bytes(const cast_kv_cache_t* cache, const cast_kv_
  *
  * q        bf16 [n_tok, Hq, dh] device; token t at t * q_stride elements (>= Hq * dh, multiple
  *          of 8), heads dense.  Hq a multiple of cache->H.
- * out      bf16 [n_tok, Hq, dh] device, dense (must not alias the inputs).
+ * out      bf16 [n_tok, Hq, dh] device, dense (must not alias the inputs; q itself is refused).
  * lse_out  fp32 [n_tok, Hq] device, natural log-sum-exp of the scaled logits, or NULL.
  * max_len  the longest length expected: it sets how finely keys are split, nothing else
  *          (longer sequences are computed, too, in longer pieces).  >= 1.
@@ -629,6 +632,8 @@ size_t cast_kv_attn_workspace_bytes(const cast_kv_cache_t* cache, const cast_kv_
  * workspace  NULL (every row tile runs whole), or 256-byte aligned with
  *          cast_kv_attn_workspace_bytes(...) of the same arguments; contents need no
  *          initialisation.  Calls that may overlap in time need workspaces of their own.
+ * n_tok * Hq < 2^31, and (rows / 16 + n_seq) * H < 2^30 for the n_tok * Hq / H rows of a head;
+ * fewer than 2^23 workgroups in a call.
  * Errors: CAST_ERR_NULL, CAST_ERR_SHAPE, CAST_ERR_UNSUPPORTED, CAST_ERR_WORKSPACE.
  */
 cast_status_t cast_kv_attn(const void* q, long long q_stride, int Hq, const cast_kv_cache_t* cache,

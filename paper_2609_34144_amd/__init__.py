@@ -783,6 +783,8 @@ def cast_kv_attn(q, cache: KvCache, seqs: KvSeqs, scale: float, causal: bool = T
     lib = _lib or load()
     if q.dim() != 3:
         _bad(f"q must be [n, Hq, dh], got {list(q.shape)}")
+    if window > 0x7fffffff or sinks > 0x7fffffff:
+        _bad(f"window and sinks must be below 2^31, got {window} and {sinks}")
     n, hq, dh = q.shape
     dev = cache.device
     if seqs.device != dev:

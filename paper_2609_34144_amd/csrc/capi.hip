@@ -645,7 +645,7 @@ static cast_status_t seqs_sizes(const cast_kv_seqs_t* s, int page, const char* w
   if (s == nullptr) return fail(CAST_ERR_NULL, "%s: seqs is NULL", who);
   if (s->n_seq < 1 || s->n_tok < 0 || s->max_pages < 1)
     return fail(CAST_ERR_SHAPE, "%s: need n_seq, max_pages >= 1 and n_tok >= 0 (got %d %d %d)", who, s->n_seq, s->max_pages, s->n_tok);
-  if (s->n_seq > (1 << 20) || s->n_tok >= (1 << 30) || s->max_pages >= (1 << 24) ||
+  if (s->n_seq > (1 << 20) || s->n_tok > (1 << 25) || s->max_pages >= (1 << 24) ||
       (long long)s->max_pages * page >= (1LL << 30) || (long long)s->max_pages * page * page >= (1LL << 40) ||
       (long long)s->n_tok * page >= (1LL << 40) || s->n_tok >= (1LL << 24) * page)
     return fail(CAST_ERR_UNSUPPORTED, "%s: more sequences (2^20), rows or pages than the indexing takes", who);
@@ -760,6 +760,7 @@ cast_status_t cast_kv_attn(const void* q, long long q_stride, int Hq, const cast
   if (st == CAST_OK) st = rows_check(out, (long long)Hq * cache->dh, Hq, cache->dh, "kv_attn", "out");
   if (st != CAST_OK) return st;
   if (!aligned(lse_out, 4)) return fail(CAST_ERR_SHAPE, "kv_attn: lse_out must be 4-byte aligned");
+  if (q == out) return fail(CAST_ERR_SHAPE, "kv_attn: out is q");
   KvAttnPlan plan = make_kv_attn_plan(cache, seqs, Hq, max_len, window, sinks);
   if (workspace == nullptr) {
     plan.pieces = 1;                               // every row tile whole
@@ -770,6 +771,8 @@ cast_status_t cast_kv_attn(const void* q, long long q_stride, int Hq, const cast
     if (plan.cut() && workspace_bytes < plan.bytes)
       return fail(CAST_ERR_WORKSPACE, "kv_attn: workspace has %zu bytes, %zu needed", workspace_bytes, plan.bytes);
   }
+  if (plan.groups(cache->H) >= (1LL << 23))
+    return fail(CAST_ERR_UNSUPPORTED, "kv_attn: %lld workgroups are too many", plan.groups(cache->H));
   return launch_kv_attn(q, q_stride, Hq, *cache, *seqs, causal, std::min(window, 1 << 30), sinks, scale, out, lse_out,
                         plan, workspace, stream);
 }

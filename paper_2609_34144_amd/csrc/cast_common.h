@@ -166,13 +166,16 @@ KvSeqs make_seqs(const cast_kv_seqs_t& s, int page);
 // How a call of cast_kv_attn is cut up.  `bytes` of workspace hold this plan and that of any
 // smaller max_len.
 struct KvAttnPlan {
-  int rows;                      // rows per workgroup: 16 or 32 (few rows), 128, 256
+  int rows;                      // rows per workgroup: 16 (few rows), 128, 256
   int row_tiles;                 // at most, over all ways to share the rows out
   int pieces, piece_tiles;       // 128 and 256 rows: pieces along the keys, key tiles of each
   int target, max_items;         // few rows: pieces wanted (0: none is cut), work items at most
   int wh;                        // few rows: heads of a workgroup
   size_t part_bytes, lse_bytes, bytes;
   bool cut() const { return pieces > 1 || target > 0; }
+  long long groups(int H) const {
+    return target > 0 ? max_items : rows == 16 ? (long long)row_tiles * (H / wh) : (long long)row_tiles * H * pieces;
+  }
 };
 KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f8, long long max_len, int window,
                         int sinks, int cus);

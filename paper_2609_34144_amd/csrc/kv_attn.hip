@@ -1591,7 +1591,8 @@ KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f
   // From 17 on the half-filled tiles win: 8 of 4096 with 17 rows 46 and 31, 32 rows 58 and 32.
   // Pairs beyond 128 rows of 128 channels, if they can be cut into enough pieces to fill the
   // card: 8 of 4096 with 192 rows 51 us, 57 in tiles; 768 rows 107 and 140; but 4 of 1024
-  // with 192 rows, 64 pieces, 30 and 25.
+  // with 192 rows, 64 pieces, 30 and 25.  (Tiles below that switch
+  // have no more pieces, and so no more workspace, than pairs above it: 3/4 cus / units at most.)
   const bool pairs = dh == 128 && mean > kTileRows && units(kPairRows) * ((nt + 7) / 8) >= cus * 3 / 4;
   p.rows = mean <= kFewRows ? kFewRows : pairs ? kPairRows : kTileRows;
   p.wh = H % 4 == 0 ? 4 : H % 2 == 0 ? 2 : 1;

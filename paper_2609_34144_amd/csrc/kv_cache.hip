@@ -563,16 +563,22 @@ KvSeqs make_seqs(const cast_kv_seqs_t& s, int page) {
 cast_status_t launch_rope(const void* x, int dtype, int n, int H, int dh, long long xt, long long xh,
                           const int32_t* pos, const cast_rope_params_t& p, int transpose, void* out,
                           long long yt, long long yh, bool wide, hipStream_t stream) {
-  const Rope r = make_rope(&p, pos, transpose);
+  Rope r = make_rope(&p, pos, transpose);
   const Items it = plan_items(r.rot, r.inter, dh, wide);
-  const int bx = (n + kTok - 1) / kTok, heads = heads_per_block(bx, H, it.per_head);
-  const dim3 grid(bx, (H + heads - 1) / heads);
-  if (dtype == 0)
-    hipLaunchKernelGGL((rope_kernel<float>), grid, dim3(kThreads), 0, stream, static_cast<const float*>(x), xt, xh,
-                       static_cast<float*>(out), yt, yh, n, H, heads, r, it);
-  else
-    hipLaunchKernelGGL((rope_kernel<uint16_t>), grid, dim3(kThreads), 0, stream, static_cast<const uint16_t*>(x), xt,
-                       xh, static_cast<uint16_t*>(out), yt, yh, n, H, heads, r, it);
+  const int heads = heads_per_block((n + kTok - 1) / kTok, H, it.per_head);
+  constexpr int kMost = 1 << 25;                 // tokens of a launch, whose threads must stay below 2^32
+  for (int at = 0; at < n; at += kMost) {
+    const int m = std::min(n - at, kMost);
+    const dim3 grid((m + kTok - 1) / kTok, (H + heads - 1) / heads);
+    r.pos = pos + (long long)at * r.n_axes;
+    if (dtype == 0)
+      hipLaunchKernelGGL((rope_kernel<float>), grid, dim3(kThreads), 0, stream, static_cast<const float*>(x) + at * xt,
+                         xt, xh, static_cast<float*>(out) + at * yt, yt, yh, m, H, heads, r, it);
+    else
+      hipLaunchKernelGGL((rope_kernel<uint16_t>), grid, dim3(kThreads), 0, stream,
+                         static_cast<const uint16_t*>(x) + at * xt, xt, xh, static_cast<uint16_t*>(out) + at * yt, yt,
+                         yh, m, H, heads, r, it);
+  }
   return check_launch("rope");
 }
 
@@ -613,7 +619,7 @@ cast_status_t launch_kv_append(const cast_kv_cache_t& c, const cast_kv_seqs_t& s
     // every group of the call holds a token, or is a sequence's first or last page
     const long long groups = (long long)s.n_tok / c.page + 2ll * s.n_seq;
     const long long blocks = (long long)a.q_blocks_x * a.q_shares + groups * 2 * c.H;
-    if (blocks >= (1ll << 31)) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
+    if (blocks >= (1ll << 24)) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
     const dim3 grid((unsigned)blocks);
     if (a.r.rot == 0) hipLaunchKernelGGL(append8_kernel<0>, grid, dim3(kThreads), 0, stream, a);
     else if (a.r.inter) hipLaunchKernelGGL(append8_kernel<2>, grid, dim3(kThreads), 0, stream, a);

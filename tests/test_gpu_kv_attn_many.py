@@ -176,3 +176,20 @@ def test_many_pieces(cast_lib, dh):
     q = bf16(rng, b.n, 3, dh, scale=2.0)
     run(cast_lib, b, q, 0.1, True, what="pieces")
     run(cast_lib, b, q, 0.1, True, 3900, 60, what="pieces")
+
+
+def test_workspace_of_a_longer_bound_serves_shorter_ones(cast_lib):
+    """The workspace does not fall as max_len grows, whichever way the rows are cut."""
+    z = lambda *s, d=torch.int32: torch.zeros(s, dtype=d, device=DEV)  # noqa: E731
+    for H, g in ((1, 1), (2, 4), (8, 1), (24, 1), (64, 1)):
+        for dh in (64, 128):
+            kv = z(1, 16, H, dh, d=torch.bfloat16)
+            cache = cast_lib.KvCache(kv, kv)
+            for n_seq in (1, 3, 40):
+                seqs = cast_lib.KvSeqs(z(n_seq + 1), z(n_seq), z(n_seq, 2048))
+                for mean in (1, 20, 130, 200, 257, 600):
+                    q = z(mean * n_seq, H * g, 1, d=torch.bfloat16)
+                    for window in (0, 500):
+                        b = [cast_lib.cast_kv_attn_workspace_bytes(q, cache, seqs, max_len=m, window=window)
+                             for m in (1, 64, 300, 512, 513, 800, 1024, 1500, 2100, 4000, 9000, 32000)]
+                        assert b == sorted(b), (H, g, dh, n_seq, mean, window, b)

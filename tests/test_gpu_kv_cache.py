@@ -283,3 +283,16 @@ def test_read(cast_lib, bits, page, H, dh):
         want = O.values(codes.cpu().numpy(), e[:, None].cpu().numpy())
         fits = np.abs(want) < 2.0 ** 128
         assert np.array_equal(f64(k)[fits], want[fits])
+
+
+def test_rope_past_one_launch(cast_lib):
+    """More tokens than the threads of one launch: the last ones equal a call of their own."""
+    n, H, dh = (1 << 25) + 7, 1, 32
+    rope = cast_lib.cast_rope_params_init(32)
+    x = torch.empty((n, H, dh), dtype=torch.bfloat16, device="cuda")
+    x[:100] = torch.randn((100, H, dh), device="cuda").bfloat16()
+    x[-100:] = torch.randn((100, H, dh), device="cuda").bfloat16()
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    out = cast_lib.cast_rope(x, pos, rope)
+    for part in (slice(0, 100), slice(n - 100, n)):
+        assert torch.equal(out[part], cast_lib.cast_rope(x[part].clone(), pos[part].clone(), rope))

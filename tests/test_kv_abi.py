@@ -219,3 +219,21 @@ def test_binding_refusals(lib):
         with pytest.raises(cast.CastError):
             f()
             print("not refused:", i)
+
+
+def test_refusals_of_sizes_that_no_launch_takes(lib):
+    """More threads than a launch holds, and an output that is the query."""
+    assert attn(lib, cache(H=4096, dh=32), seqs(n_seq=1 << 16, n_tok=1 << 16), Hq=4096, qs=4096 * 32) == UNSUPPORTED
+    assert append(lib, cache(dtype=2, k_exp=A, v_exp=A, page=1, H=512, pages=8), seqs(n_tok=1 << 15), ks=512 * 64,
+                  vs=512 * 64) == UNSUPPORTED
+    assert append(lib, s=seqs(n_tok=(1 << 25) + 1)) == UNSUPPORTED
+    assert attn(lib, out=A, q=A) == SHAPE
+
+
+def test_binding_refuses_windows_past_int32():
+    z = lambda *s, d=torch.int32: torch.zeros(s, dtype=d)  # noqa: E731
+    kv = z(4, 16, 2, 64, d=torch.bfloat16)
+    q, c, s = z(3, 2, 64, d=torch.bfloat16), cast.KvCache(kv, kv.clone()), cast.KvSeqs(z(2), z(1), z(1, 2))
+    for kw in (dict(window=1 << 32), dict(window=8, sinks=1 << 31)):
+        with pytest.raises(cast.CastError, match="below 2\\^31"):
+            cast.cast_kv_attn(q, c, s, 0.1, **kw)
