@@ -119,10 +119,22 @@ __device__ __forceinline__ void rotate_item(const T* x, T* y, int i, int mode, i
   }
 }
 
-// a (cos, sin) of a reduced angle.  v_cos and v_sin take revolutions; over [-0.5, 0.5] they
-// are off by at most 1.3e-7 (all multiples of 2^-24 against fp64), about one fp32 step of 1.
-__device__ __forceinline__ f32x2 cos_sin(float revs, float amp) {
-  return f32x2{__builtin_amdgcn_cosf(revs) * amp, __builtin_amdgcn_sinf(revs) * amp};
+// a (cos, sin) of a reduced angle: the quarter turn k and the rest r of [-1/8, 1/8], where
+//   sin(2 pi r) = r (2 pi + P(r^2)),  cos(2 pi r) = 1 + r^2 Q(r^2)
+// with P and Q fitted over that range to less than 1e-8 (2 pi in two parts).  Off by at most
+// 7.5e-8, about one fp32 step of 1.  v_cos and v_sin of an fp32 angle are off by up to 2.2e-7:
+// they put 18 of the 15 million codes of 15000 tokens of 8 heads on the other side of a
+// rounding, this 9 (means of six caches), and took 60 us for 64 with the pages read back.
+__device__ __forceinline__ f32x2 cos_sin(double revs, float amp) {
+  const float kf = rintf(4.0f * (float)revs);
+  const float r = (float)fma(-0.25, (double)kf, revs), s = r * r;
+  const float p = fmaf(fmaf(fmaf(-75.7257843f, s, 81.5995178f), s, -41.3416977f), s, -1.74845553e-7f);
+  const float q = fmaf(fmaf(fmaf(59.4235306f, s, -85.4488068f), s, 64.9393692f), s, -19.7392082f);
+  const float sn = fmaf(r, 6.28318548f, r * p), cn = fmaf(s, q, 1.0f);
+  const unsigned k = (unsigned)(int)kf;
+  const float c = (k & 1) ? sn : cn, d = (k & 1) ? cn : sn;
+  return f32x2{__uint_as_float(__float_as_uint(c) ^ (((k + 1) & 2) << 30)) * amp,
+               __uint_as_float(__float_as_uint(d) ^ ((k & 2) << 30)) * amp};
 }
 
 // (cos, sin) of the block's tokens' pairs into LDS: token of the block tt, position of axis

@@ -69,9 +69,9 @@ __device__ __forceinline__ int rope_axis(const Rope& r, int j) {
 // The angle of pair j at position p, in revolutions of [-0.5, 0.5]: the product and its
 // reduction are fp64 (fp32 would keep no angle at all of p = 10^6 and turns ~ 0.16: its
 // product is off by 2^-24 * 1.6e5 = 0.01 revolutions).
-__device__ __forceinline__ float rope_revs(double turns, int p) {
+__device__ __forceinline__ double rope_revs(double turns, int p) {
   const double t = (double)p * turns;
-  return (float)(t - rint(t));
+  return t - rint(t);
 }
 
 }  // namespace cast
