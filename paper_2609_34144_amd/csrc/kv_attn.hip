@@ -12,13 +12,20 @@
 // e4m3 codes become bf16 on the way (exactly: their scales are powers of two), so both
 // cache types share everything after the load.
 //
-// Two kernels:
-//   tiles  128 rows per workgroup; its four waves share 64-key tiles in LDS, copied one
-//          tile ahead.  Bound by the matrix cores and the softmax's VALU work.
-//   rows   16 or 32 rows per workgroup (few rows: decoding); each wave takes every fourth
-//          32-key tile by itself, keys straight from memory into MFMA operands, values through
-//          a private LDS tile; no barrier until the four results are joined.  Bound by HBM.
-// Long key ranges with few row tiles are cut into pieces, joined by a second kernel.
+// Three kernels, chosen by the rows of a sequence (kv_attn_plan):
+//   rows   16 rows per workgroup (decoding).  Its waves take neighbouring heads and walk key
+//          tiles by themselves, keys straight from memory into MFMA operands, values through
+//          a private LDS tile; no barrier until the results are joined.  Bound by HBM:
+//          16 streams of up to 8192 bf16 keys (288 MB) 55 us, 4 of up to 131072 e4m3 keys
+//          (819 MB) 154 us, 5.2 and 5.3 TB/s; their joins 7 and 10 us.
+//   tiles  128 rows per workgroup; its four waves share 64-key tiles in LDS, copied one tile
+//          ahead.  Bound by the softmax's VALU work: chunks of 64-wide heads 144 us, 700
+//          TFLOP/s (VALU 57% of the cycles, matrix cores 30%).
+//   pairs  256 rows of 128 channels per workgroup, its waves in two groups that take turns on
+//          the matrix cores and the VALU.  28160 keys by 4 x 3520 rows of 24 heads 1090
+//          TFLOP/s; 13000 causal rows of prompts up to 4096 long, 28 key tiles a workgroup,
+//          361 us, 830 TFLOP/s (matrix cores 38%: start and end of a workgroup lie bare).
+// Long key ranges with few row tiles are cut into pieces, joined by a further kernel.
 #include <algorithm>
 #include <utility>
 
@@ -59,7 +66,7 @@ constexpr int kVmcnt0 = 0x0F70;
 // (see softmax): probabilities reach 2^16, where sums of 2^24 keys of values below 2^80 are
 // still far from overflow, and the exponent's argument is off by 2^-21 at most.  With 2^8,
 // keys whose logits spread by 6 moved some wave's maximum in nearly every tile (chunks of
-// 64-wide heads 177 us, so 143; the frame over an 8-bit window 167 and 146).
+// 64-wide heads 177 us, so 144; the frame over an 8-bit window 167 and 145).
 constexpr float kMaxSlack = 16.0f;
 constexpr float kSumBound = 65536.0f;   // 2^kMaxSlack
 // "no key seen yet": below every finite scaled score, so the first visible key moves it
@@ -1031,8 +1038,8 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
 // rows
 // ---------------------------------------------------------------------------
 // v_mfma_f32_16x16x32_bf16: of 16 rows an accumulator takes a quarter of the registers that
-// 32x32 tiles need, which leaves room for three workgroups per compute unit, each wave with
-// a whole key tile on its way.
+// 32x32 tiles need, which leaves room for two workgroups per compute unit (three of narrow
+// heads), each wave with a whole key tile on its way.
 //
 // The four waves take wh = 4, 2 or 1 neighbouring heads (whatever divides H) and share each
 // head's key tiles 4 / wh ways.  Waves that walk the same tokens in step read them whole
