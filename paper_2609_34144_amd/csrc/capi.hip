@@ -763,8 +763,7 @@ cast_status_t cast_kv_attn(const void* q, long long q_stride, int Hq, const cast
   if (q == out) return fail(CAST_ERR_SHAPE, "kv_attn: out is q");
   KvAttnPlan plan = make_kv_attn_plan(cache, seqs, Hq, max_len, window, sinks);
   if (workspace == nullptr) {
-    plan.pieces = 1;                               // every row tile whole
-    plan.target = 0;
+    plan.target = 0;                               // every row tile whole
   } else {
     if (!aligned(workspace, kWsAlign))
       return fail(CAST_ERR_WORKSPACE, "kv_attn: workspace must be %zu-byte aligned", kWsAlign);

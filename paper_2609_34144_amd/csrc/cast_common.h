@@ -168,13 +168,15 @@ KvSeqs make_seqs(const cast_kv_seqs_t& s, int page);
 struct KvAttnPlan {
   int rows;                      // rows per workgroup: 16 (few rows), 128, 256
   int row_tiles;                 // at most, over all ways to share the rows out
-  int pieces, piece_tiles;       // 128 and 256 rows: pieces along the keys, key tiles of each
-  int target, max_items;         // few rows: pieces wanted (0: none is cut), work items at most
+  int target;                    // pieces wanted (0: none is cut)
+  int pieces, slabs, least;      // 128 and 256 rows: pieces of a row tile at like lengths, at most; their key tiles at least
+  int max_items;                 // few rows: work items at most
   int wh;                        // few rows: heads of a workgroup
   size_t part_bytes, lse_bytes, bytes;
-  bool cut() const { return pieces > 1 || target > 0; }
+  bool cut() const { return target > 0; }
   long long groups(int H) const {
-    return target > 0 ? max_items : rows == 16 ? (long long)row_tiles * (H / wh) : (long long)row_tiles * H * pieces;
+    if (rows == 16) return target > 0 ? max_items : (long long)row_tiles * (H / wh);
+    return (long long)row_tiles * H + target;
   }
 };
 KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f8, long long max_len, int window,

@@ -59,7 +59,7 @@ constexpr int row_keys(int dh, bool f8) { return dh == 128 && !f8 ? 32 : 64; }
 // its workgroups per compute unit (waves per SIMD)
 constexpr int row_groups(int dh) { return dh < 128 ? 3 : 2; }
 constexpr int kMaxPieces = 128;
-constexpr int kJoinWays = 8;   // threads that share the pieces of a row, from as many pieces on
+constexpr int kJoinWays = 8;   // threads that share the pieces of a row, from as many pieces on (at like lengths)
 // s_waitcnt vmcnt(0) that leaves expcnt and lgkmcnt free
 constexpr int kVmcnt0 = 0x0F70;
 // The running maximum moves only when a tile exceeds it by more than this, in log2 units
@@ -83,15 +83,15 @@ struct KvAttnArgs {
   KvSeqs s;
   uint16_t* out;
   float* lse;
-  float* part_o;                 // normalised: [pieces][n_tok * Hq][dh], or [items][wh][rows][dh]
-  float* part_lse;               // log2 domain: [pieces][n_tok * Hq], or [items][wh][rows]
+  float* part_o;                 // normalised: [slabs][n_tok * Hq][dh], or [items][wh][rows][dh]
+  float* part_lse;               // log2 domain: [slabs][n_tok * Hq], or [items][wh][rows]
   int Hq, H, g, pages, page;
   int causal, window, sinks;     // window 0: none
-  int npieces, piece_tiles;      // tiles kernel: pieces along the keys, key tiles of each
-  int row_tiles;
-  int target, max_items;         // rows kernel: pieces wanted (0: none is cut), items at most
+  int slabs, least;              // tiles kernels: pieces of a row tile at most, key tiles of a piece at least
+  int target, max_items;         // pieces wanted (0: none is cut); rows kernel: work items at most
   int wh, hgroups;               // rows kernel: heads of a workgroup (1, 2 or 4), H / wh
   int2* meta;                    // rows kernel: first item and pieces of [row tile][head group]
+  int* cuts;                     // tiles kernels: pieces of [n_tok * Hq]
   float sl2;                     // scale * log2(e)
 };
 
@@ -162,19 +162,23 @@ template <int TM>
 __device__ __forceinline__ int first_tile(const KvAttnArgs& a, int b) {
   return (int)((unsigned)(seq_row(a.s, b) * a.g) / (unsigned)TM) + b;
 }
-// row tile k of sequence b
+// row tile k of sequence b, which has call rows beg .. beg + n and is len long
 template <int TM, int TK>
-__device__ __forceinline__ bool place(const KvAttnArgs& a, int b, int k, RowTile& t) {
+__device__ __forceinline__ bool place(const KvAttnArgs& a, int b, int beg, int n, int len, int k, RowTile& t) {
   t.b = b;
-  t.beg = seq_row(a.s, b);
-  const int n = max(seq_row(a.s, b + 1) - t.beg, 0);
+  t.beg = beg;
   t.n_rows = n * a.g;
   if (k < 0 || (long long)k * TM >= t.n_rows) return false;
   t.row0 = k * TM;
-  t.len = seq_len(a.s, b);
+  t.len = len;
   t.off = t.len - n;
   key_tiles<TK>(a, t, t.off + t.row0 / a.g, t.off + (min(t.row0 + TM, t.n_rows) - 1) / a.g, t.len);
   return true;
+}
+template <int TM, int TK>
+__device__ __forceinline__ bool place(const KvAttnArgs& a, int b, int k, RowTile& t) {
+  const int beg = seq_row(a.s, b);
+  return place<TM, TK>(a, b, beg, max(seq_row(a.s, b + 1) - beg, 0), seq_len(a.s, b), k, t);
 }
 // x-th row tile of the call
 template <int TM, int TK>
@@ -182,13 +186,6 @@ __device__ __forceinline__ bool row_tile(const KvAttnArgs& a, int x, RowTile& t)
   const int b = find_seq(a.s.n_seq, x, [&](int i) { return first_tile<TM>(a, i); });
   return place<TM, TK>(a, b, x - first_tile<TM>(a, b), t);
 }
-// logical key tiles [u0, u1) of piece z
-__device__ __forceinline__ void piece_range(const KvAttnArgs& a, int nt, int z, int& u0, int& u1) {
-  const int per = max(a.piece_tiles, (nt + a.npieces - 1) / a.npieces);
-  u0 = min(z * per, nt);
-  u1 = min(u0 + per, nt);
-}
-
 // Sums over a wave by row shifts and broadcasts in the registers (shuffles go through the LDS
 // and take ten times as long): inclusive prefix sums of the lanes.
 template <int CTRL, int ROWS, class T>
@@ -206,41 +203,113 @@ __device__ __forceinline__ T prefix_sum(T v) {
 }
 __device__ __forceinline__ int lane_value(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
 
-// The head, piece and row tile of a workgroup of the tiles kernels.  The grid has room for
-// every way to share the rows out among the sequences; the row tiles that are there are
-// counted, so that the workgroups with nothing to do are the last ones of the grid.  (With a
-// spare row tile numbered after each sequence's, 512 rows over 16384 keys of 8 heads took 81
-// us and 511 rows, which need no spare one, 58: while the idle ones start and leave, others
-// pile up on the compute units that are free.)
-// Workgroup b runs on XCD b mod 8.  Each XCD takes a run of the (head, piece, row tile) list,
-// so the row tiles that read the same keys share its L2, and walks it from the end: of causal
-// rows the last tiles are the longest, and the shortest should finish the call.  (With heads
-// over all XCDs and short tiles first: prompts 463 us for 425, chunks of 64-wide heads 232
-// for 195.)
+// A sequence of the call: its rows and length, its row tiles and the key tiles they meet.
+struct SeqWork {
+  int beg, n, len, rt, nt;
+};
 template <int TM, int TK>
-__device__ __forceinline__ bool my_unit(const KvAttnArgs& a, int& z, int& h, RowTile& t) {
+__device__ __forceinline__ SeqWork seq_work(const KvAttnArgs& a, int b) {
+  SeqWork w{0, 0, 0, 0, 0};
+  if (b >= a.s.n_seq) return w;
+  w.beg = seq_row(a.s, b);
+  w.n = max(seq_row(a.s, b + 1) - w.beg, 0);
+  w.len = seq_len(a.s, b);
+  if (w.n == 0) return w;
+  w.rt = (w.n * a.g + TM - 1) / TM;
+  if (a.target == 0) return w;                       // (nt is for those who cut)
+  RowTile t;
+  key_tiles<TK>(a, t, w.len - w.n, w.len - 1, w.len);
+  w.nt = t.nt;
+  return w;
+}
+// The key tiles of a piece with which the call, `groups` times over, makes about a.target of
+// them, at most target + groups row tiles.  FIT (the tiles kernels, where a piece more than the
+// card holds costs a whole round): the first of this mean and three larger sizes that makes at
+// most a.target, else the largest.  `w` is the lane's first sequence.
+template <int TM, int TK, bool FIT>
+__device__ __forceinline__ int piece_tiles(const KvAttnArgs& a, const SeqWork& w, int groups, int least) {
   const int lane = threadIdx.x & 63;
-  auto count = [&](int b) __attribute__((always_inline)) -> int {
-    return b < a.s.n_seq ? (max(seq_row(a.s, b + 1) - seq_row(a.s, b), 0) * a.g + TM - 1) / TM : 0;
+  float sum = 0.0f;
+  for (int c = 0; c < a.s.n_seq; c += 64) {
+    const SeqWork v = c == 0 ? w : seq_work<TM, TK>(a, c + lane);
+    sum += (float)v.rt * (float)v.nt;
+  }
+  sum = __int_as_float(lane_value(__float_as_int(prefix_sum(sum)), 63));
+  const int mean = max(least, (int)fminf(ceilf(sum * (float)groups * (FIT ? 0.9999f : 1.0001f) / (float)a.target), 1.0e7f));
+  if constexpr (!FIT) return mean;
+  int per[4], n[4];
+  float inv[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    per[i] = mean + ((mean * i * (i + 3) + 31) >> 5);   // 1, 1.125, 1.31, 1.56 times
+    inv[i] = __builtin_amdgcn_rcpf((float)per[i]);
+    n[i] = 0;
+  }
+  for (int c = 0; c < a.s.n_seq; c += 64) {
+    const SeqWork v = c == 0 ? w : seq_work<TM, TK>(a, c + lane);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n[i] += v.rt * max(1, (int)ceilf((float)v.nt * inv[i] - 1e-3f));   // (near enough to choose by)
+  }
+  int best = per[3];
+#pragma unroll
+  for (int i = 2; i >= 0; --i) best = (long long)lane_value(prefix_sum(n[i]), 63) * groups <= a.target ? per[i] : best;
+  return best;
+}
+
+// The work of a workgroup of the tiles kernels: row tile, head, and the logical key tiles
+// [u0, u1), which are piece z of `pieces`.  The grid has room for every way to share the rows
+// out among the sequences; what is there is counted, so that the workgroups with nothing to
+// do are the last ones of the grid.  (With a spare row tile numbered after each sequence's,
+// 512 rows over 16384 keys of 8 heads took 81 us and 511 rows, which need no spare one, 58:
+// while the idle ones start and leave, others pile up on the compute units that are free.)
+// Workgroup b runs on XCD b mod 8.  Each XCD takes a run of the (head, sequence, piece, row
+// tile) list, so the row tiles that read the same keys share its L2, and walks it from the
+// end: of causal rows the last tiles are the longest, and the shortest should finish the call.
+// (With heads over all XCDs and short tiles first: prompts 463 us for 425, chunks of 64-wide
+// heads 232 for 195.)
+struct Unit {
+  RowTile t;
+  int h, z, pieces, u0, u1;
+};
+template <int TM, int TK>
+__device__ __forceinline__ bool my_unit(const KvAttnArgs& a, Unit& un) {
+  const int lane = threadIdx.x & 63;
+  SeqWork w = seq_work<TM, TK>(a, lane);
+  int per = 0x3fffffff;
+  if (a.target > 0) per = piece_tiles<TM, TK, true>(a, w, a.H, a.least);
+  // (slabs: a sequence much longer than the others is cut no finer than they allow)
+  auto pieces_of = [&](const SeqWork& v) __attribute__((always_inline)) -> int {
+    return a.target > 0 ? min(max(1, (v.nt + per - 1) / per), a.slabs) : 1;
   };
-  const int first = count(lane);
   int total = 0;
-  for (int c = 0; c < a.s.n_seq; c += 64) total += lane_value(prefix_sum(c == 0 ? first : count(c + lane)), 63);
-  total = min(max(total, 0), a.row_tiles);           // (the bound, whatever the offsets hold)
-  const int n = total * a.H * a.npieces, b = blockIdx.x, x = b & 7, j = b >> 3, per = n >> 3, rest = n & 7;
-  const int mine = per + (x < rest ? 1 : 0);
+  for (int c = 0; c < a.s.n_seq; c += 64) {
+    const SeqWork v = c == 0 ? w : seq_work<TM, TK>(a, c + lane);
+    total += lane_value(prefix_sum(v.rt * pieces_of(v)), 63);
+  }
+  const int grid = gridDim.x;
+  total = min(max(total, 0), grid / a.H);            // (the bound, whatever the offsets hold)
+  const int n = total * a.H, b = blockIdx.x, x = b & 7, j = b >> 3, share = n >> 3, rest = n & 7;
+  const int mine = share + (x < rest ? 1 : 0);
   if (j >= mine) return false;
-  const int unit = x * per + min(x, rest) + mine - 1 - j;
-  const int q = unit / total, rt = unit - q * total;
-  h = q / a.npieces;
-  z = q - h * a.npieces;
+  const int unit = x * share + min(x, rest) + mine - 1 - j;
+  un.h = unit / total;
+  const int at = unit - un.h * total;
   int base = 0;
   for (int c = 0; c < a.s.n_seq; c += 64) {
-    const int there = c == 0 ? first : count(c + lane), incl = prefix_sum(there);
-    const unsigned long long hit = __ballot(rt - base < incl);
+    if (c > 0) w = seq_work<TM, TK>(a, c + lane);
+    const int pieces = pieces_of(w), there = w.rt * pieces, incl = prefix_sum(there);
+    const unsigned long long hit = __ballot(at - base < incl);
     if (hit != 0) {
       const int l = __ffsll((long long)hit) - 1;
-      return place<TM, TK>(a, c + l, rt - base - lane_value(incl - there, l), t);
+      const int rt = lane_value(w.rt, l), local = at - base - lane_value(incl - there, l);
+      un.pieces = lane_value(pieces, l);
+      un.z = local / max(rt, 1);
+      if (!place<TM, TK>(a, c + l, lane_value(w.beg, l), lane_value(w.n, l), lane_value(w.len, l), local - un.z * rt, un.t))
+        return false;
+      const int size = a.target > 0 ? (lane_value(w.nt, l) + un.pieces - 1) / un.pieces : un.t.nt;
+      un.u0 = (int)min((long long)un.z * size, (long long)un.t.nt);
+      un.u1 = min(un.u0 + min(size, un.t.nt), un.t.nt);
+      return true;
     }
     base += lane_value(incl, 63);
   }
@@ -463,14 +532,15 @@ __device__ __forceinline__ void put4(const KvAttnArgs& a, long long row, int dh,
 
 // A lane's row of a tiles kernel: normalised into the output, or as piece z of it.
 template <int DH, int ND>
-__device__ __forceinline__ void finish(const KvAttnArgs& a, int z, long long row, int hf, bool any, float m_run,
+__device__ __forceinline__ void finish(const KvAttnArgs& a, const Unit& un, long long row, int hf, bool any, float m_run,
                                        float l_run, const f32x16 (&acc)[ND]) {
   const float l = l_run + __shfl_xor(l_run, 32);
   const bool some = l != 0.0f;               // true for NaN, too
   const float inv = some ? 1.0f / l : 0.0f;
   const float l2 = some ? m_run + __log2f(l) : -INFINITY;
-  const long long at = (long long)z * a.s.n_tok * a.Hq + row;
-  if (a.npieces > 1) {
+  const long long at = (long long)un.z * a.s.n_tok * a.Hq + row;
+  if (a.target > 0 && un.z == 0 && hf == 0) a.cuts[row] = un.pieces;
+  if (un.pieces > 1) {
     if (hf == 0) a.part_lse[at] = l2;
     if (!any) return;
   } else if (a.lse != nullptr && hf == 0) {
@@ -482,7 +552,7 @@ __device__ __forceinline__ void finish(const KvAttnArgs& a, int z, long long row
     for (int g4 = 0; g4 < 4; ++g4) {
       const f32x4 o{acc[db][4 * g4] * inv, acc[db][4 * g4 + 1] * inv, acc[db][4 * g4 + 2] * inv, acc[db][4 * g4 + 3] * inv};
       const int d = db * 32 + 8 * g4 + 4 * hf;
-      if (a.npieces > 1) *reinterpret_cast<f32x4*>(a.part_o + at * DH + d) = o;
+      if (un.pieces > 1) *reinterpret_cast<f32x4*>(a.part_o + at * DH + d) = o;
       else put4(a, row, DH, d, o);
     }
 }
@@ -508,14 +578,13 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
   __shared__ __attribute__((aligned(1024))) uint16_t lds_v0[TK * DH];
   __shared__ __attribute__((aligned(1024))) uint16_t lds_v1[TK * DH];
 
-  int z, h;
-  RowTile t;
-  if (!my_unit<kTileRows, TK>(a, z, h, t)) return;
+  Unit un;
+  if (!my_unit<kTileRows, TK>(a, un)) return;
+  const RowTile& t = un.t;
+  const int h = un.h, u0 = un.u0, u1 = un.u1;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hf = lane >> 5;
-  int u0, u1;
-  piece_range(a, t.nt, z, u0, u1);
 
   // the lane's row; rows past the end repeat the last one and are not stored
   const int w0 = t.row0 + wave * 32;
@@ -712,7 +781,7 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
   }
 
   if (w0 + l32 < t.n_rows)
-    finish<DH>(a, z, (long long)(t.beg + tok) * a.Hq + hq, hf, u0 < u1, m_run, l_run, acc);
+    finish<DH>(a, un, (long long)(t.beg + tok) * a.Hq + hq, hf, u0 < u1, m_run, l_run, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -739,14 +808,13 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
   __shared__ __attribute__((aligned(1024))) uint16_t lds_v1[TK * DH];
   __shared__ __attribute__((aligned(1024))) uint16_t lds_zero[TK * DH];   // values of a tile that was not seen
 
-  int z, h;
-  RowTile t;
-  if (!my_unit<kPairRows, TK>(a, z, h, t)) return;
+  Unit un;
+  if (!my_unit<kPairRows, TK>(a, un)) return;
+  const RowTile& t = un.t;
+  const int h = un.h, u0 = un.u0, u1 = un.u1;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = wave >> 2, l32 = lane & 31, hf = lane >> 5;
-  int u0, u1;
-  piece_range(a, t.nt, z, u0, u1);
 
   const int w0 = t.row0 + wave * 32;
   const bool live = w0 < t.n_rows;
@@ -1031,7 +1099,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
     if (grp == 0) __syncthreads();           // B's extra interval at the start
   }
   if (w0 + l32 < t.n_rows)
-    finish<DH>(a, z, (long long)(t.beg + tok) * a.Hq + hq, hf, n > 0, m_run, l_run, acc);
+    finish<DH>(a, un, (long long)(t.beg + tok) * a.Hq + hq, hf, n > 0, m_run, l_run, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -1058,36 +1126,12 @@ struct Item {
   int hg, z, pieces, item0;      // head group, piece of `pieces`, item of piece 0 (the next: + hgroups)
   int tile_id, per;              // number of the row tile in the call, key tiles of a piece
 };
-struct SeqWork {
-  int rt, nt;
-};
-template <int TM, int TK>
-__device__ __forceinline__ SeqWork seq_work(const KvAttnArgs& a, int b) {
-  SeqWork w{0, 0};
-  if (b >= a.s.n_seq) return w;
-  const int beg = seq_row(a.s, b), n = seq_row(a.s, b + 1) - beg, len = seq_len(a.s, b);
-  if (n <= 0) return w;
-  w.rt = (n * a.g + TM - 1) / TM;
-  RowTile t;
-  key_tiles<TK>(a, t, len - n, len - 1, len);
-  w.nt = t.nt;
-  return w;
-}
 template <int TM, int TK>
 __device__ __forceinline__ bool find_item(const KvAttnArgs& a, int x, Item& it) {
   const int lane = threadIdx.x & 63, n_seq = a.s.n_seq;
   SeqWork w = seq_work<TM, TK>(a, lane);
   int per = 0x3fffffff;
-  if (a.target > 0) {
-    float sum = 0.0f;
-    for (int c = 0; c < n_seq; c += 64) {
-      const SeqWork v = c == 0 ? w : seq_work<TM, TK>(a, c + lane);
-      sum += (float)v.rt * (float)v.nt;
-    }
-    sum = __int_as_float(lane_value(__float_as_int(prefix_sum(sum)), 63));
-    // (rounded up, so that the items never pass target + row tiles * hgroups)
-    per = max(kMinWaveKeys / TK * (kThreads / 64 / a.wh), (int)fminf(ceilf(sum * (float)a.hgroups * 1.0001f / (float)a.target), 1.0e9f));
-  }
+  if (a.target > 0) per = piece_tiles<TM, TK, false>(a, w, a.hgroups, kMinWaveKeys / TK * (kThreads / 64 / a.wh));
   int base = 0;
   for (int c = 0; c < n_seq; c += 64) {
     if (c > 0) w = seq_work<TM, TK>(a, c + lane);
@@ -1098,14 +1142,14 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, int x, Item& it) 
       const int l = __ffsll((long long)hit) - 1;
       const int first = base + lane_value(incl - mine, l);
       it.pieces = lane_value(pieces, l);
-      it.per = per;
+      it.per = a.target > 0 ? (lane_value(w.nt, l) + it.pieces - 1) / it.pieces : per;   // (even pieces)
       const int local = x - first, rest = local / a.hgroups;
       it.hg = local - rest * a.hgroups;
       const int k = rest / it.pieces;
       it.z = rest - k * it.pieces;
       it.item0 = first + k * it.pieces * a.hgroups + it.hg;
       it.tile_id = first_tile<TM>(a, c + l) + k;
-      return place<TM, TK>(a, c + l, k, it.t);
+      return place<TM, TK>(a, c + l, lane_value(w.beg, l), lane_value(w.n, l), lane_value(w.len, l), k, it.t);
     }
     base += lane_value(incl, 63);
   }
@@ -1485,8 +1529,8 @@ __global__ __launch_bounds__(kThreads) void kv_rows_join_kernel(KvAttnArgs a) {
   if (a.lse != nullptr && d == 0) a.lse[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
 }
 
-// Join of the pieces of every row, as above.  WAYS threads share the pieces of four channels
-// of a row.
+// Join of the pieces of every row that the tiles kernels cut, as above.  WAYS threads share
+// the pieces of four channels of a row.
 template <int DH, int WAYS>
 __global__ __launch_bounds__(kThreads) void kv_join_kernel(KvAttnArgs a) {
   constexpr int PER = DH / 4, ROWS = kThreads / (PER * WAYS);
@@ -1498,9 +1542,12 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(KvAttnArgs a) {
   const bool there = row < rows;
   const float* lse = a.part_lse + (there ? row : 0);
   const float* o_z = a.part_o + (there ? row : 0) * DH + d;
-  float m = -INFINITY;
+  // (rows of no sequence hold whatever lies in the workspace; they are left alone below)
+  const float early = there && way < a.slabs ? lse[way * rows] : -INFINITY;
+  const int pieces = there ? min(a.cuts[row], a.slabs) : 0;
+  float m = way < pieces ? early : -INFINITY;
 #pragma unroll 4
-  for (int z = way; z < a.npieces; z += WAYS) {
+  for (int z = way + WAYS; z < pieces; z += WAYS) {
     const float l = lse[z * rows];
     m = l > m || l != l ? l : m;
   }
@@ -1516,7 +1563,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(KvAttnArgs a) {
   float w = 0.0f;
   f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-  for (int z = way; z < a.npieces; z += WAYS) {
+  for (int z = way; z < pieces; z += WAYS) {
     const float l = lse[z * rows];
     const f32x4 p = *reinterpret_cast<const f32x4*>(o_z + z * rows * DH);
     const float c = l == m ? 1.0f : __builtin_amdgcn_exp2f(l - m);
@@ -1536,7 +1583,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(KvAttnArgs a) {
       o += part[tid + k * PER];
     }
   }
-  if (!there) return;
+  if (pieces < 2) return;                          // whole, and written
   const int tok = (int)(row / a.Hq);
   if (tok < seq_row(a.s, 0) || tok >= seq_row(a.s, a.s.n_seq)) return;   // of no sequence: left alone
   const bool some = w != 0.0f;
@@ -1562,7 +1609,7 @@ void launch_rows(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
 
 template <int DH, bool F8, bool RUNS>
 void launch_tiles(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
-  const dim3 grid(p.row_tiles * a.H * p.pieces);
+  const dim3 grid((p.row_tiles * a.H) + p.target);
   if constexpr (DH == 128) {
     if (p.rows == kPairRows) {
       hipLaunchKernelGGL((kv_pairs_kernel<F8, RUNS>), grid, dim3(kPairThreads), 0, stream, a);
@@ -1577,8 +1624,8 @@ void launch_as(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
   if (p.rows == kFewRows) return launch_rows<DH, F8>(a, p, stream);
   if (a.page % copy_rows(DH) == 0) launch_tiles<DH, F8, true>(a, p, stream);
   else launch_tiles<DH, F8, false>(a, p, stream);
-  if (p.pieces >= kJoinWays) launch_join<DH, kJoinWays>(a, stream);
-  else if (p.pieces > 1) launch_join<DH, 1>(a, stream);
+  if (p.target > 0 && p.pieces >= kJoinWays) launch_join<DH, kJoinWays>(a, stream);
+  else if (p.target > 0) launch_join<DH, 1>(a, stream);
 }
 
 }  // namespace
@@ -1592,21 +1639,21 @@ KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f
   const long long nt = (keys + kTileKeys - 1) / kTileKeys;
   auto units = [&](long long tile_rows) { return n_seq * ((mean + tile_rows - 1) / tile_rows) * H; };
   // Rows per workgroup, by their mean over the sequences (8 heads of 128 in bf16 unless said).
-  // Up to 16, the rows kernel, whose pieces follow the lengths: 16 streams of 300 to 8100
-  // tokens 63 us, as 128-row tiles 81; 4 streams of 65536 to 131072 e4m3 tokens 164 and 298.
-  // (Of sequences of one length tiles would gain: 8 of 4096 tokens with 16 rows 41 and 31.)
-  // From 17 on the half-filled tiles win: 8 of 4096 with 17 rows 46 and 31, 32 rows 58 and 32.
+  // The rows kernel up to 16 of codes, which the tiles kernel widens once for 128 rows, for
+  // few as for many (one sequence of 131072: 64 us, as 128-row tiles 86), and of bf16 where
+  // nothing is cut (256 of 512 tokens 94 and 117); else up to 8 (16 streams of 300 to 8100
+  // tokens, 4 rows 63 and 69; 16 rows 64 and 50; 8 of 4096, 16 rows 40 and 32).
+  // From 17 on the half-filled tiles win: 8 of 4096, 17 rows 46 us and 30, 32 rows 58 and 32.
   // Pairs beyond 128 rows of 128 channels, if they can be cut into enough pieces to fill the
   // card: 8 of 4096 with 192 rows 51 us, 57 in tiles; 768 rows 107 and 140; but 4 of 1024
-  // with 192 rows, 64 pieces, 30 and 25.  (Tiles below that switch
-  // have no more pieces, and so no more workspace, than pairs above it: 3/4 cus / units at most.)
+  // with 192 rows, 64 pieces, 30 and 25.  (Tiles below that switch have no more pieces, and so
+  // no more workspace, than pairs above it: 3/4 cus / units at most.)
   const bool pairs = dh == 128 && mean > kTileRows && units(kPairRows) * ((nt + 7) / 8) >= cus * 3 / 4;
-  p.rows = mean <= kFewRows ? kFewRows : pairs ? kPairRows : kTileRows;
+  const int few = f8 || units(kTileRows) > cus ? kFewRows : kFewRows / 2;
+  p.rows = mean <= few ? kFewRows : pairs ? kPairRows : kTileRows;
   p.wh = H % 4 == 0 ? 4 : H % 2 == 0 ? 2 : 1;
   // at most, over all ways to share the rows out
   p.row_tiles = (int)(p.rows == kFewRows ? rows / p.rows + n_seq : (rows + (long long)n_seq * (p.rows - 1)) / p.rows);
-  p.pieces = 1;
-  p.piece_tiles = 1;
   if (cus <= 0 || n_tok < 1) return p;
   if (p.rows < kTileRows) {
     // workgroups resident at once, less the partial pieces that the row tiles end with
@@ -1619,17 +1666,20 @@ KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f
     p.bytes = p.part_bytes + p.lse_bytes + align_up((size_t)p.row_tiles * (H / p.wh) * sizeof(int2));
     return p;
   }
-  const long long want = (long long)cus * (p.rows == kPairRows ? 1 : 2) / std::max(units(p.rows), 1ll);
+  const long long resident = (long long)cus * (p.rows == kPairRows ? 1 : 2), items = units(p.rows);
   // Key tiles of a piece: a piece of few rows leaves little to join (48 rows over 4 x 1024
   // keys: 17 us with 4 tiles at least, 22 with 8; 128 rows over 16384: 48 and 36).
-  const long long least = std::clamp(mean / 16, 4ll, 8ll);
-  const long long most = std::min<long long>(std::min<long long>(want, kMaxPieces), (nt + least - 1) / least);
-  if (most < 2) return p;
-  p.piece_tiles = (int)((nt + most - 1) / most);
-  p.pieces = (int)((nt + p.piece_tiles - 1) / p.piece_tiles);
-  p.part_bytes = align_up((size_t)most * n_tok * H * g * dh * 4);
-  p.lse_bytes = align_up((size_t)most * n_tok * H * g * 4);
-  p.bytes = p.part_bytes + p.lse_bytes;
+  p.least = (int)std::clamp(mean / 16, 4ll, 8ll);
+  // A sequence is cut into at most four times as many pieces as all would be at one length.
+  const long long want = resident / std::max(items, 1ll);
+  const long long most = std::min<long long>(kMaxPieces, (nt + p.least - 1) / p.least);
+  p.pieces = (int)std::min(want, most);
+  if (p.pieces < 2) return p;
+  p.slabs = (int)std::min(4 * want, most);
+  p.target = (int)resident;
+  p.part_bytes = align_up((size_t)p.slabs * n_tok * H * g * dh * 4);
+  p.lse_bytes = align_up((size_t)p.slabs * n_tok * H * g * 4);
+  p.bytes = p.part_bytes + p.lse_bytes + align_up((size_t)n_tok * H * g * 4);
   return p;
 }
 
@@ -1649,6 +1699,7 @@ cast_status_t launch_kv_attn(const void* q, long long q_stride, int Hq, const ca
   a.part_o = static_cast<float*>(workspace);
   a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.part_bytes);
   a.meta = reinterpret_cast<int2*>(static_cast<char*>(workspace) + plan.part_bytes + plan.lse_bytes);
+  a.cuts = reinterpret_cast<int*>(a.meta);
   a.wh = plan.wh;
   a.hgroups = c.H / plan.wh;
   a.target = plan.target;
@@ -1661,9 +1712,8 @@ cast_status_t launch_kv_attn(const void* q, long long q_stride, int Hq, const ca
   a.causal = causal;
   a.window = window;
   a.sinks = window > 0 ? sinks : 0;
-  a.npieces = plan.pieces;
-  a.row_tiles = plan.row_tiles;
-  a.piece_tiles = plan.piece_tiles;
+  a.slabs = plan.slabs;
+  a.least = plan.least;
   a.sl2 = scale * 1.4426950408889634f;
   const bool f8 = c.dtype == 2;
   switch (c.dh) {
