@@ -13,19 +13,22 @@
 // cache types share everything after the load.
 //
 // Three kernels, chosen by the rows of a sequence (kv_attn_plan):
-//   rows   16 rows per workgroup (decoding).  Its waves take neighbouring heads and walk key
-//          tiles by themselves, keys straight from memory into MFMA operands, values through
-//          a private LDS tile; no barrier until the results are joined.  Bound by HBM:
-//          16 streams of up to 8192 bf16 keys (288 MB) 55 us, 4 of up to 131072 e4m3 keys
-//          (819 MB) 154 us, 5.2 and 5.3 TB/s; their joins 7 and 10 us.
+//   rows   16 rows per workgroup (decoding; of bf16 up to 8 where keys are cut).  Its waves
+//          take neighbouring heads and walk key tiles by themselves, keys straight from
+//          memory into MFMA operands, values through a private LDS tile; no barrier until the
+//          results are joined.  Bound by HBM: 16 streams of up to 8192 bf16 keys (288 MB) 54
+//          us, 4 of up to 131072 e4m3 keys (819 MB) 154 us, 5.3 TB/s; their joins 7 and 10 us.
 //   tiles  128 rows per workgroup; its four waves share 64-key tiles in LDS, copied one tile
 //          ahead.  Bound by the softmax's VALU work: chunks of 64-wide heads 144 us, 700
 //          TFLOP/s (VALU 57% of the cycles, matrix cores 30%).
 //   pairs  256 rows of 128 channels per workgroup, its waves in two groups that take turns on
 //          the matrix cores and the VALU.  28160 keys by 4 x 3520 rows of 24 heads 1090
 //          TFLOP/s; 13000 causal rows of prompts up to 4096 long, 28 key tiles a workgroup,
-//          361 us, 830 TFLOP/s (matrix cores 38%: start and end of a workgroup lie bare).
-// Long key ranges with few row tiles are cut into pieces, joined by a further kernel.
+//          361 to 372 us, 805 to 830 TFLOP/s (matrix cores 38%: start and end of a workgroup
+//          lie bare).
+// Long key ranges with few row tiles are cut into pieces by the lengths the device sees (16
+// streams of 400 to 8192 keys, 64 rows of each: 116 us cut by the bound on the lengths, 94
+// so); a further kernel joins them.
 #include <algorithm>
 #include <utility>
 
