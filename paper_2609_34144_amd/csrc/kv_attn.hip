@@ -307,6 +307,7 @@ __device__ __forceinline__ bool my_unit(const KvAttnArgs& a, Unit& un) {
       const int rt = lane_value(w.rt, l), local = at - base - lane_value(incl - there, l);
       un.pieces = lane_value(pieces, l);
       un.z = local / max(rt, 1);
+      if (local < 0 || un.z >= un.pieces) return false;   // (sums that wrapped: offsets that hold garbage)
       if (!place<TM, TK>(a, c + l, lane_value(w.beg, l), lane_value(w.n, l), lane_value(w.len, l), local - un.z * rt, un.t))
         return false;
       const int size = a.target > 0 ? (lane_value(w.nt, l) + un.pieces - 1) / un.pieces : un.t.nt;
@@ -1147,6 +1148,7 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, int x, Item& it) 
       it.pieces = lane_value(pieces, l);
       it.per = a.target > 0 ? (lane_value(w.nt, l) + it.pieces - 1) / it.pieces : per;   // (even pieces)
       const int local = x - first, rest = local / a.hgroups;
+      if (local < 0) return false;                   // (sums that wrapped: offsets that hold garbage)
       it.hg = local - rest * a.hgroups;
       const int k = rest / it.pieces;
       it.z = rest - k * it.pieces;
