@@ -124,19 +124,18 @@ __device__ __forceinline__ void rotate_item(const T* x, T* y, int i, int mode, i
   }
 }
 
-// a (cos, sin) of a reduced angle: the quarter turn k and the rest r of [-1/8, 1/8], where
+// a (cos, sin) of an angle.  Of the rest of a quarter turn, r of [-1/8, 1/8] in turns,
 //   sin(2 pi r) = r (2 pi + P(r^2)),  cos(2 pi r) = 1 + r^2 Q(r^2)
 // with P and Q fitted over that range to less than 1e-8 (2 pi in two parts).  Off by at most
 // 7.5e-8, about one fp32 step of 1.  v_cos and v_sin of an fp32 angle are off by up to 2.2e-7:
 // they put 18 of the 15 million codes of 15000 tokens of 8 heads on the other side of a
 // rounding, this 9 (means of six caches), and took 60 us for 64 with the pages read back.
-__device__ __forceinline__ f32x2 cos_sin(double revs, float amp) {
-  const float kf = rintf(4.0f * (float)revs);
-  const float r = (float)fma(-0.25, (double)kf, revs), s = r * r;
+__device__ __forceinline__ f32x2 cos_sin(Angle t, float amp) {
+  const float r = 0.25f * t.r, s = r * r;
   const float p = fmaf(fmaf(fmaf(-75.7257843f, s, 81.5995178f), s, -41.3416977f), s, -1.74845553e-7f);
   const float q = fmaf(fmaf(fmaf(59.4235306f, s, -85.4488068f), s, 64.9393692f), s, -19.7392082f);
   const float sn = fmaf(r, 6.28318548f, r * p), cn = fmaf(s, q, 1.0f);
-  const unsigned k = (unsigned)(int)kf;
+  const unsigned k = (unsigned)t.k;
   const float c = (k & 1) ? sn : cn, d = (k & 1) ? cn : sn;
   return f32x2{__uint_as_float(__float_as_uint(c) ^ (((k + 1) & 2) << 30)) * amp,
                __uint_as_float(__float_as_uint(d) ^ ((k & 2) << 30)) * amp};
@@ -150,7 +149,7 @@ __device__ __forceinline__ void fill_angles(f32x2 (*cs)[kMaxPairs], const Rope& 
   for (int t = threadIdx.x; t < kTok * kMaxPairs; t += kThreads) {
     const int tt = t / kMaxPairs, j = t % kMaxPairs;
     if (j < pairs) {
-      const f32x2 c = cos_sin(rope_revs(r.turns[j], pos_of(tt, rope_axis(r, j))), r.amp);
+      const f32x2 c = cos_sin(rope_angle(quarter_turns(r.turns[j]), pos_of(tt, rope_axis(r, j))), r.amp);
       cs[tt][j] = f32x2{c.x, c.y * r.sign};
     }
   }
@@ -350,7 +349,7 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
       const int ch = c0 + e;
       const int j = MODE == 1 ? ch : MODE == 2 ? (c0 >> 1) + e : ch >= half ? ch - half : ch;
       const int jj = min(j, half - 1);
-      freq[e] = r.turns[jj];
+      freq[e] = quarter_turns(r.turns[jj]);
       axes |= (uint32_t)rope_axis(r, jj) << (2 * e);
     }
   }
@@ -371,7 +370,7 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
       const int32_t* pos = r.pos != nullptr ? r.pos + (long long)(g.row0 + t) * r.n_axes : nullptr;
       const int p0 = pos != nullptr ? pos[0] : g.index0 + t;
       auto angle = [&](int e) {
-        return cos_sin(rope_revs(freq[e], r.n_axes > 1 && pos != nullptr ? pos[(axes >> (2 * e)) & 3] : p0), r.amp);
+        return cos_sin(rope_angle(freq[e], r.n_axes > 1 && pos != nullptr ? pos[(axes >> (2 * e)) & 3] : p0), r.amp);
       };
       const uint16_t* row = g.src + t * g.ss;
 #pragma unroll

@@ -66,12 +66,19 @@ __device__ __forceinline__ int rope_axis(const Rope& r, int j) {
   return r.axis == nullptr ? 0 : min((int)r.axis[j], r.n_axes - 1);
 }
 
-// The angle of pair j at position p, in revolutions of [-0.5, 0.5]: the product and its
-// reduction are fp64 (fp32 would keep no angle at all of p = 10^6 and turns ~ 0.16: its
-// product is off by 2^-24 * 1.6e5 = 0.01 revolutions).
-__device__ __forceinline__ double rope_revs(double turns, int p) {
-  const double t = (double)p * turns;
-  return t - rint(t);
+// The angle of a pair at position p: k quarter turns and the rest r of one, r in [-0.5, 0.5].
+// Whole turns of `turns` go first, so p times the rest stays below 2^33 quarters, whose
+// integer part the addition of 1.5 * 2^52 leaves in the sum's low bits; r is rounded once.
+// (In fp32 p = 10^6 and turns ~ 0.16 would leave no angle at all: 2^-24 * 1.6e5 = 0.01 turns.)
+struct Angle {
+  int k;
+  float r;
+};
+__device__ __forceinline__ double quarter_turns(double turns) { return 4.0 * (turns - rint(turns)); }
+__device__ __forceinline__ Angle rope_angle(double quarters, int p) {
+  constexpr double kInt = 6755399441055744.0;    // 1.5 * 2^52
+  const double t = fma((double)p, quarters, kInt);
+  return Angle{(int)__double_as_longlong(t), (float)fma((double)p, quarters, kInt - t)};
 }
 
 }  // namespace cast
