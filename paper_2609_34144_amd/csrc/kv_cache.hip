@@ -3,8 +3,8 @@
 // latency of one launch): every value is read once, converted in registers, written once.
 // 28160 tokens of 24 heads of 128 channels rotated: 66 us, 5.2 TB/s; 24960 tokens of 12 heads
 // appended in bf16: 62 us, 4.9 TB/s; 15000 tokens of 8 heads in e4m3, half of the channels
-// rotated: 32 us, 2.9 TB/s (the angles' fp64 and the two passes over a page take as long as
-// the memory), read back as bf16 29 us; 16 e4m3 pages of 3520 tokens of 24 heads read: 171 us,
+// rotated: 28 us, 3.3 TB/s (the angles and the two passes over a page take as long as the
+// memory), read back as bf16 29 us; 16 e4m3 pages of 3520 tokens of 24 heads read: 171 us,
 // 6.1 TB/s.
 #include <algorithm>
 
@@ -129,7 +129,7 @@ __device__ __forceinline__ void rotate_item(const T* x, T* y, int i, int mode, i
 // with P and Q fitted over that range to less than 1e-8 (2 pi in two parts).  Off by at most
 // 7.5e-8, about one fp32 step of 1.  v_cos and v_sin of an fp32 angle are off by up to 2.2e-7:
 // they put 18 of the 15 million codes of 15000 tokens of 8 heads on the other side of a
-// rounding, this 9 (means of six caches), and took 60 us for 64 with the pages read back.
+// rounding, this 9 (means of six caches), and took 60 us for 64 with the pages read back (61 since heads share angles).
 __device__ __forceinline__ f32x2 cos_sin(Angle t, float amp) {
   const float r = 0.25f * t.r, s = r * r;
   const float p = fmaf(fmaf(fmaf(-75.7257843f, s, 81.5995178f), s, -41.3416977f), s, -1.74845553e-7f);
@@ -143,10 +143,10 @@ __device__ __forceinline__ f32x2 cos_sin(Angle t, float amp) {
 
 // (cos, sin) of the block's tokens' pairs into LDS: token of the block tt, position of axis
 // a given by pos_of(tt, a).
-template <class F>
+template <int T = kThreads, class F>
 __device__ __forceinline__ void fill_angles(f32x2 (*cs)[kMaxPairs], const Rope& r, F&& pos_of) {
   const int pairs = r.rot >> 1;
-  for (int t = threadIdx.x; t < kTok * kMaxPairs; t += kThreads) {
+  for (int t = threadIdx.x; t < kTok * kMaxPairs; t += T) {
     const int tt = t / kMaxPairs, j = t % kMaxPairs;
     if (j < pairs) {
       const f32x2 c = cos_sin(rope_angle(quarter_turns(r.turns[j]), pos_of(tt, rope_axis(r, j))), r.amp);
@@ -220,6 +220,7 @@ __device__ __forceinline__ void locate(const AppendArgs& a, int row, int* index,
 
 // Heads are counted K 0 .. H, V .. 2 H, Q .. 2 H + Hq; block (x, y) takes kTok tokens and
 // the heads [y heads, (y + 1) heads) of that count, from `first` on.
+template <int T>
 __device__ __forceinline__ void append_rows(const AppendArgs& a, int bx, int by, int first,
                                             f32x2 (*cs)[kMaxPairs], int* index, int* slot, int* mine) {
   const int t0 = bx * kTok, n = a.s.n_tok, nt = min(kTok, n - t0);
@@ -227,7 +228,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int bx, int by,
   if (wave < nt) locate(a, t0 + wave, index + wave, slot + wave, mine + wave);
   __syncthreads();
   if (a.r.rot > 0) {
-    fill_angles(cs, a.r, [&](int tt, int ax) {
+    fill_angles<T>(cs, a.r, [&](int tt, int ax) {
       const int t = min(tt, nt - 1);
       return a.r.pos != nullptr ? a.r.pos[(long long)(t0 + t) * a.r.n_axes + ax] : index[t];
     });
@@ -236,7 +237,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int bx, int by,
   const int h0 = first + by * a.heads, nh = min(a.heads, 2 * a.H + a.Hq - h0);
   const int per_tok = nh * a.it.per_head;
   const long long row = (long long)a.H * a.dh;
-  for (int i = threadIdx.x; i < nt * per_tok; i += kThreads) {
+  for (int i = threadIdx.x; i < nt * per_tok; i += T) {
     const int tt = i / per_tok, rem = i - tt * per_tok;
     int h = div_by(rem, a.it.div);
     const int item = rem - h * a.it.per_head;
@@ -277,7 +278,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int bx, int by,
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   __shared__ f32x2 cs[kTok][kMaxPairs];
   __shared__ int index[kTok], slot[kTok], mine[kTok];
-  append_rows(a, blockIdx.x, blockIdx.y, 0, cs, index, slot, mine);
+  append_rows<kThreads>(a, blockIdx.x, blockIdx.y, 0, cs, index, slot, mine);
 }
 
 // ---------------------------------------------------------------------------
@@ -326,10 +327,10 @@ struct PageRows {
   int had, n, row0, index0;      // earlier tokens, new ones; first call row and index in the sequence
 };
 constexpr int kKeep = 2;
-template <int MODE>
-__device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int dh, float* tops) {
+template <int MODE, int NH, int T>
+__device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int dh, float (*tops)[T / 64]) {
   const int ipr = dh >> 4, shift = 31 - __clz(ipr);            // items per row
-  const int item = threadIdx.x & (ipr - 1), t0 = threadIdx.x >> shift, step = kThreads >> shift;
+  const int item = threadIdx.x & (ipr - 1), t0 = threadIdx.x >> shift, step = T >> shift;
   const int half = r.rot >> 1;
   int c0 = 16 * item, c1 = c0 + 8;               // first channels of the item's chunks
   bool turns = MODE != 0 && c0 < r.rot;
@@ -353,18 +354,24 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
       axes |= (uint32_t)rope_axis(r, jj) << (2 * e);
     }
   }
-  auto fetch = [&](int base, float (&y)[kKeep][16]) __attribute__((always_inline)) {
-    u32x4 w[kKeep][2];
+  auto fetch = [&](int base, float (&y)[NH][kKeep][16]) __attribute__((always_inline)) {
+    u32x4 w[NH][kKeep][2];
 #pragma unroll
     for (int j = 0; j < kKeep; ++j) {
       const uint16_t* row = g.src + min(base + t0 + j * step, g.n - 1) * g.ss;
-      w[j][0] = *reinterpret_cast<const u32x4*>(row + c0);
-      w[j][1] = *reinterpret_cast<const u32x4*>(row + c1);
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        w[h][j][0] = *reinterpret_cast<const u32x4*>(row + h * dh + c0);
+        w[h][j][1] = *reinterpret_cast<const u32x4*>(row + h * dh + c1);
+      }
     }
 #pragma unroll
     for (int j = 0; j < kKeep; ++j) {
-      unpack8(w[j][0], y[j]);
-      unpack8(w[j][1], y[j] + 8);
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        unpack8(w[h][j][0], y[h][j]);
+        unpack8(w[h][j][1], y[h][j] + 8);
+      }
       if (MODE == 0 || !turns) continue;
       const int t = min(base + t0 + j * step, g.n - 1);
       const int32_t* pos = r.pos != nullptr ? r.pos + (long long)(g.row0 + t) * r.n_axes : nullptr;
@@ -379,48 +386,67 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
           const int ch = c0 + e;
           if (ch < r.rot) {
             const f32x2 a = angle(e);
-            const float o = to_f32(row[ch < half ? ch + half : ch - half]);
-            y[j][e] = fmaf(y[j][e], a.x, ch < half ? -(o * a.y) : o * a.y);
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
+              const float o = to_f32(row[h * dh + (ch < half ? ch + half : ch - half)]);
+              y[h][j][e] = fmaf(y[h][j][e], a.x, ch < half ? -(o * a.y) : o * a.y);
+            }
           }
         } else {
           const int u = MODE == 1 ? e : 2 * e, z = MODE == 1 ? 8 + e : 2 * e + 1;
           if (MODE == 1 || c0 + 2 * e < r.rot) {
             const f32x2 a = angle(e);
-            const float yu = y[j][u], yz = y[j][z];
-            y[j][u] = fmaf(yu, a.x, -(yz * a.y));
-            y[j][z] = fmaf(yu, a.y, yz * a.x);
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
+              const float yu = y[h][j][u], yz = y[h][j][z];
+              y[h][j][u] = fmaf(yu, a.x, -(yz * a.y));
+              y[h][j][z] = fmaf(yu, a.y, yz * a.x);
+            }
           }
         }
       }
     }
   };
-  float top = 0.0f;
-  auto look = [&](const float (&y)[kKeep][16]) __attribute__((always_inline)) {   // (repeated last rows do no harm)
+  float top[NH];
 #pragma unroll
-    for (int j = 0; j < kKeep; ++j)
+  for (int h = 0; h < NH; ++h) top[h] = 0.0f;
+  auto look = [&](const float (&y)[NH][kKeep][16]) __attribute__((always_inline)) {   // (repeated last rows do no harm)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float m = fabsf(y[j][e]);
-        top = m < INFINITY ? fmaxf(top, m) : top;   // false for NaN, too
-      }
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int j = 0; j < kKeep; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float m = fabsf(y[h][j][e]);
+          top[h] = m < INFINITY ? fmaxf(top[h], m) : top[h];   // false for NaN, too
+        }
   };
-  const int old = min((int)*g.exponent, 247) - 127;
+  int old[NH];
+#pragma unroll
+  for (int h = 0; h < NH; ++h) old[h] = min((int)g.exponent[h], 247) - 127;
   const int batch = kKeep * step;
-  float keep[kKeep][16];
+  float keep[NH][kKeep][16];
 #pragma unroll 1
   for (int base = 0; base < g.n; base += batch) {
     fetch(base, keep);
     look(keep);
   }
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-  __syncthreads();                               // (also: every thread has read the old exponent)
+  for (int h = 0; h < NH; ++h) {
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) top = fmaxf(top, tops[w]);
-  const int need = need_exp(top), e = g.had > 0 ? max(old, need) : need;
-  if (threadIdx.x == 0) *g.exponent = (uint8_t)(e + 127);
-  const float inv = exp_scale(-e);
+    for (int d = 32; d > 0; d >>= 1) top[h] = fmaxf(top[h], __shfl_xor(top[h], d));
+    if ((threadIdx.x & 63) == 0) tops[h][threadIdx.x >> 6] = top[h];
+  }
+  __syncthreads();                               // (also: every thread has read the old exponents)
+  int ex[NH];
+#pragma unroll
+  for (int h = 0; h < NH; ++h) {
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) top[h] = fmaxf(top[h], tops[h][w]);
+    const int need = need_exp(top[h]);
+    ex[h] = g.had > 0 ? max(old[h], need) : need;
+    if (threadIdx.x == 0) g.exponent[h] = (uint8_t)(ex[h] + 127);
+  }
 #pragma unroll 1
   for (int base = 0; base < g.n; base += batch) {
     if (g.n > batch) fetch(base, keep);
@@ -430,19 +456,25 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
       if (t < g.n) {
         uint8_t* at = g.page + (g.had + t) * g.cs;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const float* y = &keep[j][8 * k];
-          *reinterpret_cast<u32x2*>(at + (k == 0 ? c0 : c1)) =
-              u32x2{codes4(y[0], y[1], y[2], y[3], inv), codes4(y[4], y[5], y[6], y[7], inv)};
+        for (int h = 0; h < NH; ++h) {
+          const float inv = exp_scale(-ex[h]);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float* y = &keep[h][j][8 * k];
+            *reinterpret_cast<u32x2*>(at + h * dh + (k == 0 ? c0 : c1)) =
+                u32x2{codes4(y[0], y[1], y[2], y[3], inv), codes4(y[4], y[5], y[6], y[7], inv)};
+          }
         }
       }
     }
   }
   // earlier tokens of the page, rounded to the larger exponent
-  if (g.had > 0 && e > old) {
-    const float down = e - old < 127 ? exp_scale(old - e) : 0.0f;
+#pragma unroll
+  for (int h = 0; h < NH; ++h) {
+    if (g.had == 0 || ex[h] <= old[h]) continue;
+    const float down = ex[h] - old[h] < 127 ? exp_scale(old[h] - ex[h]) : 0.0f;
     for (int t = t0; t < g.had; t += step) {
-      u32x4* at = reinterpret_cast<u32x4*>(g.page + t * g.cs + 16 * item);
+      u32x4* at = reinterpret_cast<u32x4*>(g.page + t * g.cs + h * dh + 16 * item);
       const u32x4 w = *at;
       u32x4 o;
 #pragma unroll
@@ -455,23 +487,24 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
   }
 }
 
-// One block per (page of a sequence that the call writes, head, K or V).  The call's pages
+// One block per (page of a sequence that the call writes, head of V or NH heads of K, which
+// share their angles).  The call's pages
 // of sequence b are numbered from cu[b] / page + 2 b (a sequence of n tokens meets at most
 // ceil(n / page) + 1 pages, so the ranges do not meet).  KM: how keys are rotated.
-template <int KM>
-__global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a) {
+template <int KM, int NH, int T>
+__global__ __launch_bounds__(T) void append8_kernel(AppendArgs a) {
   __shared__ f32x2 cs[kTok][kMaxPairs];
   __shared__ int index[kTok], slot[kTok], mine[kTok];
-  __shared__ float tops[kThreads / 64];
+  __shared__ float tops[NH][T / 64];
   const int nq = a.q_blocks_x * a.q_shares;
   if ((int)blockIdx.x < nq) {
-    append_rows(a, blockIdx.x % a.q_blocks_x, blockIdx.x / a.q_blocks_x, 2 * a.H, cs, index, slot, mine);
+    append_rows<T>(a, blockIdx.x % a.q_blocks_x, blockIdx.x / a.q_blocks_x, 2 * a.H, cs, index, slot, mine);
     return;
   }
   const int unit = blockIdx.x - nq;
-  const int x = unit / (2 * a.H), rem = unit - x * 2 * a.H;
-  const bool is_v = rem >= a.H;
-  const int h = is_v ? rem - a.H : rem;
+  const int groups = a.H / NH, x = unit / (groups + a.H), rem = unit - x * (groups + a.H);
+  const bool is_v = rem >= groups;
+  const int h = is_v ? rem - groups : rem * NH;
   const int b = find_seq(a.s.n_seq, x, [&](int i) { return div_by(seq_row(a.s, i), a.s.page) + 2 * i; });
   const int beg = seq_row(a.s, b), end = seq_row(a.s, b + 1), len = seq_len(a.s, b);
   const int first = max(len - (end - beg), 0);   // rows before token 0 are dropped
@@ -490,8 +523,8 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a) {
   g.cs = (long long)a.H * a.dh;
   g.page = static_cast<uint8_t*>(is_v ? a.vc : a.kc) + ((long long)id * a.page * a.H + h) * a.dh;
   g.exponent = (is_v ? a.ve : a.ke) + (long long)id * a.H + h;
-  if (is_v) store_page<0>(a.r, g, a.dh, tops);
-  else store_page<KM>(a.r, g, a.dh, tops);
+  if (is_v) store_page<0, 1, T>(a.r, g, a.dh, tops);
+  else store_page<KM, NH, T>(a.r, g, a.dh, tops);
 }
 
 // ---------------------------------------------------------------------------
@@ -559,6 +592,11 @@ Rope make_rope(const cast_rope_params_t* p, const int32_t* pos, int transpose) {
   r.amp = p->amplitude;
   r.sign = transpose ? -1.0f : 1.0f;
   return r;
+}
+
+template <int KM, int NH, int T>
+void launch_append8(const AppendArgs& a, dim3 grid, hipStream_t stream) {
+  hipLaunchKernelGGL((append8_kernel<KM, NH, T>), grid, dim3(T), 0, stream, a);
 }
 
 // heads per block: all of them once there are blocks for every compute unit several
@@ -634,13 +672,30 @@ cast_status_t launch_kv_append(const cast_kv_cache_t& c, const cast_kv_seqs_t& s
     }
     // every group of the call holds a token, or is a sequence's first or last page
     const long long groups = (long long)s.n_tok / c.page + 2ll * s.n_seq;
-    const long long blocks = (long long)a.q_blocks_x * a.q_shares + groups * 2 * c.H;
-    if (blocks >= (1ll << 24)) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
+    // A thread of kThreads keeps its rows of `batch` tokens in registers.  Longer pages are
+    // read twice, by blocks of 1024 threads (512 where partners are read one by one, for the
+    // registers), as the block of a page's head works alone: a frame of 1560 tokens and 12
+    // heads that fills a page 57 us, 97 with 256 threads; 16 of them 120 and 133.
+    // Two heads of K to a block where that leaves a thousand: 15000 tokens of 8 heads in
+    // pages of 64 29 us and 25.5; but 8 x 512 tokens 10.8 and 11.4, 300 x 2 in pages of 100 11 and 13.
+    const int batch = kKeep * kThreads * 16 / c.dh;
+    const bool longp = c.page > batch;
+    const int mode = a.r.rot == 0 ? 0 : a.r.inter ? 2 : a.r.rot % 16 == 0 ? 1 : 3;
+    const int nh = (mode == 1 || mode == 2) && !longp && c.H % 2 == 0 && groups * c.H >= 1024 ? 2 : 1;
+    const long long blocks = (long long)a.q_blocks_x * a.q_shares + groups * (c.H + c.H / nh);
+    if (blocks >= (1ll << (longp ? 22 : 24))) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
     const dim3 grid((unsigned)blocks);
-    if (a.r.rot == 0) hipLaunchKernelGGL(append8_kernel<0>, grid, dim3(kThreads), 0, stream, a);
-    else if (a.r.inter) hipLaunchKernelGGL(append8_kernel<2>, grid, dim3(kThreads), 0, stream, a);
-    else if (a.r.rot % 16 == 0) hipLaunchKernelGGL(append8_kernel<1>, grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL(append8_kernel<3>, grid, dim3(kThreads), 0, stream, a);
+    switch (mode) {
+      case 0: longp ? launch_append8<0, 1, 1024>(a, grid, stream) : launch_append8<0, 1, kThreads>(a, grid, stream); break;
+      case 3: longp ? launch_append8<3, 1, 512>(a, grid, stream) : launch_append8<3, 1, kThreads>(a, grid, stream); break;
+      case 1:
+        if (longp) launch_append8<1, 1, 1024>(a, grid, stream);
+        else nh == 2 ? launch_append8<1, 2, kThreads>(a, grid, stream) : launch_append8<1, 1, kThreads>(a, grid, stream);
+        break;
+      default:
+        if (longp) launch_append8<2, 1, 1024>(a, grid, stream);
+        else nh == 2 ? launch_append8<2, 2, kThreads>(a, grid, stream) : launch_append8<2, 1, kThreads>(a, grid, stream);
+    }
   }
   return check_launch("kv_append");
 }
