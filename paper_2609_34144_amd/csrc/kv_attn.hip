@@ -24,7 +24,7 @@
 //   pairs  256 rows of 128 channels per workgroup, its waves in two groups that take turns on
 //          the matrix cores and the VALU.  28160 keys by 4 x 3520 rows of 24 heads 1090
 //          TFLOP/s; 13000 causal rows of prompts up to 4096 long, 28 key tiles a workgroup,
-//          361 to 372 us, 805 to 830 TFLOP/s (matrix cores 38%: start and end of a workgroup
+//          361 to 379 us, 790 to 830 TFLOP/s (matrix cores 38%: start and end of a workgroup
 //          lie bare).
 // Long key ranges with few row tiles are cut into pieces by the lengths the device sees (16
 // streams of 400 to 8192 keys, 64 rows of each: 116 us cut by the bound on the lengths, 94
