@@ -143,10 +143,10 @@ __device__ __forceinline__ f32x2 cos_sin(Angle t, float amp) {
 
 // (cos, sin) of the block's tokens' pairs into LDS: token of the block tt, position of axis
 // a given by pos_of(tt, a).
-template <int T = kThreads, class F>
+template <class F>
 __device__ __forceinline__ void fill_angles(f32x2 (*cs)[kMaxPairs], const Rope& r, F&& pos_of) {
   const int pairs = r.rot >> 1;
-  for (int t = threadIdx.x; t < kTok * kMaxPairs; t += T) {
+  for (int t = threadIdx.x; t < kTok * kMaxPairs; t += kThreads) {
     const int tt = t / kMaxPairs, j = t % kMaxPairs;
     if (j < pairs) {
       const f32x2 c = cos_sin(rope_angle(quarter_turns(r.turns[j]), pos_of(tt, rope_axis(r, j))), r.amp);
@@ -199,6 +199,7 @@ struct AppendArgs {
   int H, Hq, dh, pages, page;
   int heads;                     // heads of K, V and Q together per block
   int q_blocks_x, q_shares;      // 8-bit: blocks of the queries in front of the pages'
+  int parts, part;               // 8-bit, long pages: parts of a page, tokens of each
 };
 
 // Sequence, index in it and row of the cache (-1: none) of a call's row: one wave per row.
@@ -220,7 +221,6 @@ __device__ __forceinline__ void locate(const AppendArgs& a, int row, int* index,
 
 // Heads are counted K 0 .. H, V .. 2 H, Q .. 2 H + Hq; block (x, y) takes kTok tokens and
 // the heads [y heads, (y + 1) heads) of that count, from `first` on.
-template <int T>
 __device__ __forceinline__ void append_rows(const AppendArgs& a, int bx, int by, int first,
                                             f32x2 (*cs)[kMaxPairs], int* index, int* slot, int* mine) {
   const int t0 = bx * kTok, n = a.s.n_tok, nt = min(kTok, n - t0);
@@ -228,7 +228,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int bx, int by,
   if (wave < nt) locate(a, t0 + wave, index + wave, slot + wave, mine + wave);
   __syncthreads();
   if (a.r.rot > 0) {
-    fill_angles<T>(cs, a.r, [&](int tt, int ax) {
+    fill_angles(cs, a.r, [&](int tt, int ax) {
       const int t = min(tt, nt - 1);
       return a.r.pos != nullptr ? a.r.pos[(long long)(t0 + t) * a.r.n_axes + ax] : index[t];
     });
@@ -237,7 +237,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int bx, int by,
   const int h0 = first + by * a.heads, nh = min(a.heads, 2 * a.H + a.Hq - h0);
   const int per_tok = nh * a.it.per_head;
   const long long row = (long long)a.H * a.dh;
-  for (int i = threadIdx.x; i < nt * per_tok; i += T) {
+  for (int i = threadIdx.x; i < nt * per_tok; i += kThreads) {
     const int tt = i / per_tok, rem = i - tt * per_tok;
     int h = div_by(rem, a.it.div);
     const int item = rem - h * a.it.per_head;
@@ -278,7 +278,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int bx, int by,
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   __shared__ f32x2 cs[kTok][kMaxPairs];
   __shared__ int index[kTok], slot[kTok], mine[kTok];
-  append_rows<kThreads>(a, blockIdx.x, blockIdx.y, 0, cs, index, slot, mine);
+  append_rows(a, blockIdx.x, blockIdx.y, 0, cs, index, slot, mine);
 }
 
 // ---------------------------------------------------------------------------
@@ -327,10 +327,34 @@ struct PageRows {
   int had, n, row0, index0;      // earlier tokens, new ones; first call row and index in the sequence
 };
 constexpr int kKeep = 2;
-template <int MODE, int NH, int T>
-__device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int dh, float (*tops)[T / 64]) {
+
+// The first `rows` tokens of a page, at channel `at` from its head on, rounded to an exponent
+// that has grown by `up`.
+__device__ __forceinline__ void round_again(const PageRows& g, int at, int rows, int up, int dh) {
+  if (rows == 0 || up <= 0) return;
+  const int ipr = dh >> 4, shift = 31 - __clz(ipr), item = threadIdx.x & (ipr - 1), step = kThreads >> shift;
+  const float down = up < 127 ? exp_scale(-up) : 0.0f;
+  for (int t = threadIdx.x >> shift; t < rows; t += step) {
+    u32x4* p = reinterpret_cast<u32x4*>(g.page + t * g.cs + at + 16 * item);
+    const u32x4 w = *p;
+    u32x4 o;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
+      o[k] = codes4(lo.x, lo.y, hi.x, hi.y, down);
+    }
+    *p = o;
+  }
+}
+
+// PHASE kFind and kStore are the two passes alone, over rows that stay in registers: kFind
+// leaves the exponent that the rows need as the first byte of their first row, where kStore's
+// codes come to lie.
+enum Phase { kBoth, kFind, kStore };
+template <int MODE, int NH, int PHASE>
+__device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int dh, float (*tops)[kThreads / 64]) {
   const int ipr = dh >> 4, shift = 31 - __clz(ipr);            // items per row
-  const int item = threadIdx.x & (ipr - 1), t0 = threadIdx.x >> shift, step = T >> shift;
+  const int item = threadIdx.x & (ipr - 1), t0 = threadIdx.x >> shift, step = kThreads >> shift;
   const int half = r.rot >> 1;
   int c0 = 16 * item, c1 = c0 + 8;               // first channels of the item's chunks
   bool turns = MODE != 0 && c0 < r.rot;
@@ -429,23 +453,29 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
 #pragma unroll 1
   for (int base = 0; base < g.n; base += batch) {
     fetch(base, keep);
-    look(keep);
+    if (PHASE != kStore) look(keep);
   }
-#pragma unroll
-  for (int h = 0; h < NH; ++h) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top[h] = fmaxf(top[h], __shfl_xor(top[h], d));
-    if ((threadIdx.x & 63) == 0) tops[h][threadIdx.x >> 6] = top[h];
-  }
-  __syncthreads();                               // (also: every thread has read the old exponents)
   int ex[NH];
+  if constexpr (PHASE == kStore) {
 #pragma unroll
-  for (int h = 0; h < NH; ++h) {
+    for (int h = 0; h < NH; ++h) ex[h] = old[h];
+  } else {
 #pragma unroll
-    for (int w = 0; w < T / 64; ++w) top[h] = fmaxf(top[h], tops[h][w]);
-    const int need = need_exp(top[h]);
-    ex[h] = g.had > 0 ? max(old[h], need) : need;
-    if (threadIdx.x == 0) g.exponent[h] = (uint8_t)(ex[h] + 127);
+    for (int h = 0; h < NH; ++h) {
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) top[h] = fmaxf(top[h], __shfl_xor(top[h], d));
+      if ((threadIdx.x & 63) == 0) tops[h][threadIdx.x >> 6] = top[h];
+    }
+    __syncthreads();                             // (also: every thread has read the old exponents)
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+#pragma unroll
+      for (int w = 0; w < kThreads / 64; ++w) top[h] = fmaxf(top[h], tops[h][w]);
+      const int need = need_exp(top[h]);
+      ex[h] = PHASE == kBoth && g.had > 0 ? max(old[h], need) : need;
+      if (threadIdx.x == 0) *(PHASE == kBoth ? g.exponent + h : g.page + g.had * g.cs + h * dh) = (uint8_t)(ex[h] + 127);
+    }
+    if (PHASE == kFind) return;
   }
 #pragma unroll 1
   for (int base = 0; base < g.n; base += batch) {
@@ -468,22 +498,9 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
       }
     }
   }
-  // earlier tokens of the page, rounded to the larger exponent
+  if constexpr (PHASE == kBoth) {
 #pragma unroll
-  for (int h = 0; h < NH; ++h) {
-    if (g.had == 0 || ex[h] <= old[h]) continue;
-    const float down = ex[h] - old[h] < 127 ? exp_scale(old[h] - ex[h]) : 0.0f;
-    for (int t = t0; t < g.had; t += step) {
-      u32x4* at = reinterpret_cast<u32x4*>(g.page + t * g.cs + h * dh + 16 * item);
-      const u32x4 w = *at;
-      u32x4 o;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
-        o[k] = codes4(lo.x, lo.y, hi.x, hi.y, down);
-      }
-      *at = o;
-    }
+    for (int h = 0; h < NH; ++h) round_again(g, h * dh, g.had, ex[h] - old[h], dh);
   }
 }
 
@@ -491,29 +508,18 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
 // share their angles).  The call's pages
 // of sequence b are numbered from cu[b] / page + 2 b (a sequence of n tokens meets at most
 // ceil(n / page) + 1 pages, so the ranges do not meet).  KM: how keys are rotated.
-template <int KM, int NH, int T>
-__global__ __launch_bounds__(T) void append8_kernel(AppendArgs a) {
-  __shared__ f32x2 cs[kTok][kMaxPairs];
-  __shared__ int index[kTok], slot[kTok], mine[kTok];
-  __shared__ float tops[NH][T / 64];
-  const int nq = a.q_blocks_x * a.q_shares;
-  if ((int)blockIdx.x < nq) {
-    append_rows<T>(a, blockIdx.x % a.q_blocks_x, blockIdx.x / a.q_blocks_x, 2 * a.H, cs, index, slot, mine);
-    return;
-  }
-  const int unit = blockIdx.x - nq;
-  const int groups = a.H / NH, x = unit / (groups + a.H), rem = unit - x * (groups + a.H);
-  const bool is_v = rem >= groups;
-  const int h = is_v ? rem - groups : rem * NH;
+__device__ __forceinline__ bool page_rows(const AppendArgs& a, int unit, int nh, PageRows& g, bool& is_v) {
+  const int groups = a.H / nh, x = unit / (groups + a.H), rem = unit - x * (groups + a.H);
+  is_v = rem >= groups;
+  const int h = is_v ? rem - groups : rem * nh;
   const int b = find_seq(a.s.n_seq, x, [&](int i) { return div_by(seq_row(a.s, i), a.s.page) + 2 * i; });
   const int beg = seq_row(a.s, b), end = seq_row(a.s, b + 1), len = seq_len(a.s, b);
   const int first = max(len - (end - beg), 0);   // rows before token 0 are dropped
   const int p = div_by(first, a.s.page) + (x - (div_by(beg, a.s.page) + 2 * b));
   const int lo = max(first, p * a.page), hi = min(len, (p + 1) * a.page);
-  if (x < div_by(beg, a.s.page) + 2 * b || end <= beg || lo >= hi) return;
+  if (x < div_by(beg, a.s.page) + 2 * b || end <= beg || lo >= hi) return false;
   const int id = a.s.table[(long long)b * a.s.max_pages + p];
-  if (id < 0 || id >= a.pages) return;
-  PageRows g;
+  if (id < 0 || id >= a.pages) return false;
   g.had = lo - p * a.page;
   g.n = hi - lo;
   g.row0 = end - (len - lo);
@@ -523,8 +529,62 @@ __global__ __launch_bounds__(T) void append8_kernel(AppendArgs a) {
   g.cs = (long long)a.H * a.dh;
   g.page = static_cast<uint8_t*>(is_v ? a.vc : a.kc) + ((long long)id * a.page * a.H + h) * a.dh;
   g.exponent = (is_v ? a.ve : a.ke) + (long long)id * a.H + h;
-  if (is_v) store_page<0, 1, T>(a.r, g, a.dh, tops);
-  else store_page<KM, NH, T>(a.r, g, a.dh, tops);
+  return true;
+}
+
+template <int KM, int NH>
+__global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a) {
+  __shared__ f32x2 cs[kTok][kMaxPairs];
+  __shared__ int index[kTok], slot[kTok], mine[kTok];
+  __shared__ float tops[NH][kThreads / 64];
+  const int nq = a.q_blocks_x * a.q_shares;
+  if ((int)blockIdx.x < nq) {
+    append_rows(a, blockIdx.x % a.q_blocks_x, blockIdx.x / a.q_blocks_x, 2 * a.H, cs, index, slot, mine);
+    return;
+  }
+  PageRows g;
+  bool is_v;
+  if (!page_rows(a, blockIdx.x - nq, NH, g, is_v)) return;
+  if (is_v) store_page<0, 1, kBoth>(a.r, g, a.dh, tops);
+  else store_page<KM, NH, kBoth>(a.r, g, a.dh, tops);
+}
+
+// Long pages, in three launches: the exponents that `a.parts` blocks per page and head need
+// for `a.part` tokens each (and the queries), the page's exponent from them, the codes.
+template <int KM, int NH, int PHASE>
+__global__ __launch_bounds__(kThreads) void append8_part_kernel(AppendArgs a) {
+  __shared__ f32x2 cs[kTok][kMaxPairs];
+  __shared__ int index[kTok], slot[kTok], mine[kTok];
+  __shared__ float tops[NH][kThreads / 64];
+  const int nq = PHASE == kFind ? a.q_blocks_x * a.q_shares : 0;
+  if (PHASE == kFind && (int)blockIdx.x < nq) {
+    append_rows(a, blockIdx.x % a.q_blocks_x, blockIdx.x / a.q_blocks_x, 2 * a.H, cs, index, slot, mine);
+    return;
+  }
+  const int x = blockIdx.x - nq, unit = x / a.parts, off = (x - unit * a.parts) * a.part;
+  PageRows g;
+  bool is_v;
+  if (!page_rows(a, unit, NH, g, is_v) || off >= g.n) return;
+  g.src += off * g.ss;
+  g.had += off;
+  g.row0 += off;
+  g.index0 += off;
+  g.n = min(g.n - off, a.part);
+  if (is_v) store_page<0, 1, PHASE>(a.r, g, a.dh, tops);
+  else store_page<KM, NH, PHASE>(a.r, g, a.dh, tops);
+}
+__global__ __launch_bounds__(kThreads) void append8_exponent_kernel(AppendArgs a) {
+  PageRows g;
+  bool is_v;
+  if (!page_rows(a, blockIdx.x, 1, g, is_v)) return;
+  const int old = min((int)*g.exponent, 247) - 127;
+  __syncthreads();                               // (every thread has read it)
+  int need = 0;
+#pragma unroll 8
+  for (int off = 0; off < g.n; off += a.part) need = max(need, (int)g.page[(g.had + off) * g.cs]);
+  const int e = g.had > 0 ? max(old, need - 127) : need - 127;
+  if (threadIdx.x == 0) *g.exponent = (uint8_t)(e + 127);
+  round_again(g, 0, g.had, e - old, a.dh);
 }
 
 // ---------------------------------------------------------------------------
@@ -594,9 +654,12 @@ Rope make_rope(const cast_rope_params_t* p, const int32_t* pos, int transpose) {
   return r;
 }
 
-template <int KM, int NH, int T>
-void launch_append8(const AppendArgs& a, dim3 grid, hipStream_t stream) {
-  hipLaunchKernelGGL((append8_kernel<KM, NH, T>), grid, dim3(T), 0, stream, a);
+template <int KM, int NH>
+void launch_append8_parts(const AppendArgs& a, long long groups, hipStream_t stream) {
+  const unsigned nq = a.q_blocks_x * a.q_shares, units = (unsigned)(groups * (a.H + a.H / NH));
+  hipLaunchKernelGGL((append8_part_kernel<KM, NH, kFind>), dim3(nq + units * a.parts), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(append8_exponent_kernel, dim3((unsigned)groups * 2 * a.H), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((append8_part_kernel<KM, NH, kStore>), dim3(units * a.parts), dim3(kThreads), 0, stream, a);
 }
 
 // heads per block: all of them once there are blocks for every compute unit several
@@ -672,30 +735,35 @@ cast_status_t launch_kv_append(const cast_kv_cache_t& c, const cast_kv_seqs_t& s
     }
     // every group of the call holds a token, or is a sequence's first or last page
     const long long groups = (long long)s.n_tok / c.page + 2ll * s.n_seq;
-    // A thread of kThreads keeps its rows of `batch` tokens in registers.  Longer pages are
-    // read twice, by blocks of 1024 threads (512 where partners are read one by one, for the
-    // registers), as the block of a page's head works alone: a frame of 1560 tokens and 12
-    // heads that fills a page 57 us, 97 with 256 threads; 16 of them 120 and 133.
+    // The rows of `part` tokens stay in a block's registers.  Where sequences bring many more
+    // to longer pages, several blocks share a page and head, at the price of two more launches:
+    // a frame of 1560 tokens and 12 heads that is a page 17 us, 97 with one block each; 4 x
+    // 6240 tokens in such pages 100 and 134; but 2 x 300 in pages of 100 13.5 and 11.
     // Two heads of K to a block where that leaves a thousand: 15000 tokens of 8 heads in
-    // pages of 64 29 us and 25.5; but 8 x 512 tokens 10.8 and 11.4, 300 x 2 in pages of 100 11 and 13.
-    const int batch = kKeep * kThreads * 16 / c.dh;
-    const bool longp = c.page > batch;
+    // pages of 64 29 us and 25.5; but 8 x 512 tokens 10.8 and 11.4, 2 x 300 in pages of 100 11
+    // and 13.
+    a.part = kKeep * kThreads * 16 / c.dh;
+    a.parts = c.page > 4 * a.part && s.n_tok / s.n_seq > 2 * a.part ? (c.page + a.part - 1) / a.part : 1;
     const int mode = a.r.rot == 0 ? 0 : a.r.inter ? 2 : a.r.rot % 16 == 0 ? 1 : 3;
-    const int nh = (mode == 1 || mode == 2) && !longp && c.H % 2 == 0 && groups * c.H >= 1024 ? 2 : 1;
-    const long long blocks = (long long)a.q_blocks_x * a.q_shares + groups * (c.H + c.H / nh);
-    if (blocks >= (1ll << (longp ? 22 : 24))) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
-    const dim3 grid((unsigned)blocks);
-    switch (mode) {
-      case 0: longp ? launch_append8<0, 1, 1024>(a, grid, stream) : launch_append8<0, 1, kThreads>(a, grid, stream); break;
-      case 3: longp ? launch_append8<3, 1, 512>(a, grid, stream) : launch_append8<3, 1, kThreads>(a, grid, stream); break;
-      case 1:
-        if (longp) launch_append8<1, 1, 1024>(a, grid, stream);
-        else nh == 2 ? launch_append8<1, 2, kThreads>(a, grid, stream) : launch_append8<1, 1, kThreads>(a, grid, stream);
-        break;
-      default:
-        if (longp) launch_append8<2, 1, 1024>(a, grid, stream);
-        else nh == 2 ? launch_append8<2, 2, kThreads>(a, grid, stream) : launch_append8<2, 1, kThreads>(a, grid, stream);
+    const int nh = (mode == 1 || mode == 2) && c.H % 2 == 0 && groups * a.parts * c.H >= 1024 ? 2 : 1;
+    const long long units = groups * (c.H + c.H / nh), blocks = (long long)a.q_blocks_x * a.q_shares + units * a.parts;
+    if (blocks >= (1ll << 24)) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
+    if (a.parts > 1) {
+      if (mode == 0) launch_append8_parts<0, 1>(a, groups, stream);
+      else if (mode == 1 && nh == 2) launch_append8_parts<1, 2>(a, groups, stream);
+      else if (mode == 1) launch_append8_parts<1, 1>(a, groups, stream);
+      else if (mode == 2 && nh == 2) launch_append8_parts<2, 2>(a, groups, stream);
+      else if (mode == 2) launch_append8_parts<2, 1>(a, groups, stream);
+      else launch_append8_parts<3, 1>(a, groups, stream);
+      return check_launch("kv_append");
     }
+    const dim3 grid((unsigned)blocks);
+    if (mode == 0) hipLaunchKernelGGL((append8_kernel<0, 1>), grid, dim3(kThreads), 0, stream, a);
+    else if (mode == 1 && nh == 2) hipLaunchKernelGGL((append8_kernel<1, 2>), grid, dim3(kThreads), 0, stream, a);
+    else if (mode == 1) hipLaunchKernelGGL((append8_kernel<1, 1>), grid, dim3(kThreads), 0, stream, a);
+    else if (mode == 2 && nh == 2) hipLaunchKernelGGL((append8_kernel<2, 2>), grid, dim3(kThreads), 0, stream, a);
+    else if (mode == 2) hipLaunchKernelGGL((append8_kernel<2, 1>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((append8_kernel<3, 1>), grid, dim3(kThreads), 0, stream, a);
   }
   return check_launch("kv_append");
 }
