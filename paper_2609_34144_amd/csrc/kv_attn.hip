@@ -569,13 +569,22 @@ __device__ __forceinline__ void finish(const KvAttnArgs& a, const Unit& un, long
 // page, and their place is one number for the wave; else every lane fetches its row's place
 // from the lane that looked it up.  (The LDS, which that goes through, is as busy as the matrix cores.)
 constexpr int copy_rows(int dh) { return 1024 / dh; }
+// Codes of a tile come in 16-byte loads, dh / 16 to a row: load i of a wave covers copy_rows(dh)
+// rows from this one on.  A tile of 32-wide heads has a load for two of the four waves; the
+// others have none (-1): their rows would lie behind the tile's, which nothing looked up.
+constexpr int code_loads(int dh) { return (kTileKeys * dh / 16 + kThreads - 1) / kThreads; }
+constexpr int code_rows(int dh, int wave, int i) {
+  const int first = (wave + i * (kThreads / 64)) * copy_rows(dh);
+  return code_loads(dh) * kThreads * 16 / dh > kTileKeys && first >= kTileKeys ? -1 : first;
+}
+
 template <int DH, bool F8, bool RUNS>
 __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv_tiles_kernel(KvAttnArgs a) {
   constexpr int CPR = DH / 8, ROWB = DH * 2, ND = DH / 32, TK = kTileKeys;
   constexpr int NSLOT = DH / 32;             // 1-KB copies of a bf16 tile per wave
   constexpr int RSTEP = 2048 / DH;           // tile rows between them
   constexpr int C8 = DH / 16;                // 16-byte chunks of a row of codes
-  constexpr int N8 = (TK * C8 + kThreads - 1) / kThreads;
+  constexpr int N8 = code_loads(DH);
   // separate objects: the compiler sees that copies do not touch the buffer being read
   __shared__ __attribute__((aligned(1024))) uint16_t lds_k0[TK * DH];
   __shared__ __attribute__((aligned(1024))) uint16_t lds_k1[TK * DH];
@@ -656,13 +665,13 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
     ex = (int)a.ke[pe] | (int)a.ve[pe] << 8;
 #pragma unroll
     for (int i = 0; i < N8; ++i) {
-      const int c = tid + i * kThreads, row = min(c / C8, TK - 1);
+      const int c = tid + i * kThreads, first = code_rows(DH, wave, i);
+      if (first < 0) continue;
       long long at = head_bytes;
       if constexpr (RUNS) {
-        const int first = min(wave * (64 / C8) + i * (kThreads / C8), TK - 1);
         at += (long long)__builtin_amdgcn_readlane(slot, first) * row_bytes + (unsigned)(lane / C8 * (int)row_bytes + (lane % C8) * 16);
       } else {
-        at += (long long)__shfl(slot, row) * row_bytes + (c % C8) * 16;
+        at += (long long)__shfl(slot, c / C8) * row_bytes + (c % C8) * 16;
       }
       ck[i] = *reinterpret_cast<const u32x4*>(a.k + at);
       cv[i] = *reinterpret_cast<const u32x4*>(a.v + at);
@@ -671,19 +680,18 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
   auto store8 = [&](uint16_t* kd, uint16_t* vd) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < N8; ++i) {
-      const int c = tid + i * kThreads, row = c / C8, ch = 2 * (c % C8);
+      const int c = tid + i * kThreads, row = c / C8, ch = 2 * (c % C8), first = code_rows(DH, wave, i);
+      if (first < 0) continue;
       int e;
-      if constexpr (RUNS) e = __builtin_amdgcn_readlane(ex, min(wave * (64 / C8) + i * (kThreads / C8), TK - 1));
-      else e = __shfl(ex, min(row, TK - 1));
-      if (row < TK) {
-        const float sk = byte_scale(e & 255), sv = byte_scale(e >> 8);
-        char* kr = reinterpret_cast<char*>(kd) + row * ROWB;
-        char* vr = reinterpret_cast<char*>(vd) + row * ROWB;
-        *reinterpret_cast<u32x4*>(kr + ((ch ^ kswz(row, CPR)) * 16)) = widen8(ck[i].x, ck[i].y, sk);
-        *reinterpret_cast<u32x4*>(kr + (((ch + 1) ^ kswz(row, CPR)) * 16)) = widen8(ck[i].z, ck[i].w, sk);
-        *reinterpret_cast<u32x4*>(vr + ((ch ^ vswz(row, CPR)) * 16)) = widen8(cv[i].x, cv[i].y, sv);
-        *reinterpret_cast<u32x4*>(vr + (((ch + 1) ^ vswz(row, CPR)) * 16)) = widen8(cv[i].z, cv[i].w, sv);
-      }
+      if constexpr (RUNS) e = __builtin_amdgcn_readlane(ex, first);
+      else e = __shfl(ex, row);
+      const float sk = byte_scale(e & 255), sv = byte_scale(e >> 8);
+      char* kr = reinterpret_cast<char*>(kd) + row * ROWB;
+      char* vr = reinterpret_cast<char*>(vd) + row * ROWB;
+      *reinterpret_cast<u32x4*>(kr + ((ch ^ kswz(row, CPR)) * 16)) = widen8(ck[i].x, ck[i].y, sk);
+      *reinterpret_cast<u32x4*>(kr + (((ch + 1) ^ kswz(row, CPR)) * 16)) = widen8(ck[i].z, ck[i].w, sk);
+      *reinterpret_cast<u32x4*>(vr + ((ch ^ vswz(row, CPR)) * 16)) = widen8(cv[i].x, cv[i].y, sv);
+      *reinterpret_cast<u32x4*>(vr + (((ch + 1) ^ vswz(row, CPR)) * 16)) = widen8(cv[i].z, cv[i].w, sv);
     }
   };
 
@@ -1634,6 +1642,9 @@ void launch_as(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t stream) {
 }
 
 }  // namespace
+
+// (host code's view of code_rows, for tests)
+int kv_attn_code_rows(int dh, int wave, int i) { return i < code_loads(dh) ? code_rows(dh, wave, i) : -1; }
 
 KvAttnPlan kv_attn_plan(long long n_tok, int n_seq, int g, int H, int dh, bool f8, long long max_len, int window, int sinks,
                         int cus) {
