@@ -585,8 +585,9 @@ typedef struct {
  * 16-byte aligned tensors (int32 ones 4-byte); H <= 4096, page < 2^24,
  * pages * page < 2^31, page * H * H < 2^40; n_seq <= 2^20, n_tok <= 2^25, max_pages < 2^24,
  * max_pages * page < 2^30, max_pages * page * page and n_tok * page < 2^40, n_tok < 2^24 page
- * (the same limits hold for every call on a cache); an 8-bit cache takes fewer than 2^24
- * (page, head) pieces of K and V in a call.
+ * (the same limits hold for every call on a cache).  An 8-bit cache takes a
+ * call of fewer than 2^24 workgroups: (n_tok / page + 2 n_seq) 2 H at most for K and V, and
+ * max(n_tok / 4 + 1, 1024) for the queries.
  * Errors: CAST_ERR_NULL, CAST_ERR_SHAPE, CAST_ERR_UNSUPPORTED (dh; sizes past the limits).
  */
 cast_status_t cast_kv_append(const cast_kv_cache_t* cache, const cast_kv_seqs_t* seqs,

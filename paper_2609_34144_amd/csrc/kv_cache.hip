@@ -199,7 +199,8 @@ struct AppendArgs {
   int H, Hq, dh, pages, page;
   int heads;                     // heads of K, V and Q together per block
   int q_blocks_x, q_shares;      // 8-bit: blocks of the queries in front of the pages'
-  int parts, part;               // 8-bit, long pages: parts of a page, tokens of each
+  int part_log2;                 // 8-bit, long pages: tokens of a part
+  FastDiv page_parts;            // by the parts of a page
 };
 
 // Sequence, index in it and row of the cache (-1: none) of a call's row: one wave per row.
@@ -504,20 +505,9 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
   }
 }
 
-// One block per (page of a sequence that the call writes, head of V or NH heads of K, which
-// share their angles).  The call's pages
-// of sequence b are numbered from cu[b] / page + 2 b (a sequence of n tokens meets at most
-// ceil(n / page) + 1 pages, so the ranges do not meet).  KM: how keys are rotated.
-__device__ __forceinline__ bool page_rows(const AppendArgs& a, int unit, int nh, PageRows& g, bool& is_v) {
-  const int groups = a.H / nh, x = unit / (groups + a.H), rem = unit - x * (groups + a.H);
-  is_v = rem >= groups;
-  const int h = is_v ? rem - groups : rem * nh;
-  const int b = find_seq(a.s.n_seq, x, [&](int i) { return div_by(seq_row(a.s, i), a.s.page) + 2 * i; });
-  const int beg = seq_row(a.s, b), end = seq_row(a.s, b + 1), len = seq_len(a.s, b);
-  const int first = max(len - (end - beg), 0);   // rows before token 0 are dropped
-  const int p = div_by(first, a.s.page) + (x - (div_by(beg, a.s.page) + 2 * b));
-  const int lo = max(first, p * a.page), hi = min(len, (p + 1) * a.page);
-  if (x < div_by(beg, a.s.page) + 2 * b || end <= beg || lo >= hi) return false;
+// Rows lo .. hi of sequence b (end: its last call row + 1, len: its length), which lie in its page p.
+__device__ __forceinline__ bool rows_of(const AppendArgs& a, int b, int end, int len, int p, int lo, int hi, int h, bool is_v,
+                                        PageRows& g) {
   const int id = a.s.table[(long long)b * a.s.max_pages + p];
   if (id < 0 || id >= a.pages) return false;
   g.had = lo - p * a.page;
@@ -530,6 +520,50 @@ __device__ __forceinline__ bool page_rows(const AppendArgs& a, int unit, int nh,
   g.page = static_cast<uint8_t*>(is_v ? a.vc : a.kc) + ((long long)id * a.page * a.H + h) * a.dh;
   g.exponent = (is_v ? a.ve : a.ke) + (long long)id * a.H + h;
   return true;
+}
+// The units of a launch: a number x for the rows, times V's heads and groups of nh of K's.
+__device__ __forceinline__ int unit_rows(const AppendArgs& a, int unit, int nh, int& h, bool& is_v) {
+  const int groups = a.H / nh, x = unit / (groups + a.H), rem = unit - x * (groups + a.H);
+  is_v = rem >= groups;
+  h = is_v ? rem - groups : rem * nh;
+  return x;
+}
+
+// One block per (page of a sequence that the call writes, head of V or NH heads of K, which
+// share their angles).  The call's pages
+// of sequence b are numbered from cu[b] / page + 2 b (a sequence of n tokens meets at most
+// ceil(n / page) + 1 pages, so the ranges do not meet).  KM: how keys are rotated.
+__device__ __forceinline__ bool page_rows(const AppendArgs& a, int unit, int nh, PageRows& g, bool& is_v) {
+  int h;
+  const int x = unit_rows(a, unit, nh, h, is_v);
+  const int b = find_seq(a.s.n_seq, x, [&](int i) { return div_by(seq_row(a.s, i), a.s.page) + 2 * i; });
+  const int beg = seq_row(a.s, b), end = seq_row(a.s, b + 1), len = seq_len(a.s, b);
+  const int first = max(len - (end - beg), 0);   // rows before token 0 are dropped
+  const int p = div_by(first, a.s.page) + (x - (div_by(beg, a.s.page) + 2 * b));
+  const int lo = max(first, p * a.page), hi = min(len, (p + 1) * a.page);
+  if (x < div_by(beg, a.s.page) + 2 * b || end <= beg || lo >= hi) return false;
+  return rows_of(a, b, end, len, p, lo, hi, h, is_v, g);
+}
+
+// Long pages: parts of 2^part_log2 rows, from a page's first row on.  n tokens meet at most
+// n / part + n / page + 4 of them (n - 1 steps from token to token cross one border in a part's
+// rows but for the short last part of each page they pass, and the two at their ends), so those
+// of sequence b are numbered from cu[b] / part + cu[b] / page + 4 b: the grid goes by the tokens
+// of the call, not by what its pages could hold.
+__device__ __forceinline__ int parts_of(const AppendArgs& a, int n) { return (n >> a.part_log2) + div_by(n, a.s.page); }
+__device__ __forceinline__ bool part_rows(const AppendArgs& a, int unit, int nh, PageRows& g, bool& is_v) {
+  int h;
+  const int x = unit_rows(a, unit, nh, h, is_v);
+  const int b = find_seq(a.s.n_seq, x, [&](int i) { return parts_of(a, seq_row(a.s, i)) + 4 * i; });
+  const int beg = seq_row(a.s, b), end = seq_row(a.s, b + 1), len = seq_len(a.s, b);
+  const int j = x - (parts_of(a, beg) + 4 * b);
+  if (end <= beg || j < 0 || j >= parts_of(a, end - beg) + 4) return false;
+  const int first = max(len - (end - beg), 0), p0 = div_by(first, a.s.page);
+  const int at = p0 * a.page_parts.d + ((first - p0 * a.page) >> a.part_log2) + j;
+  const int p = div_by(at, a.page_parts), r0 = (at - p * a.page_parts.d) << a.part_log2;
+  const int lo = max(first, p * a.page + r0), hi = min(len, p * a.page + min(r0 + (1 << a.part_log2), a.page));
+  if (lo >= hi) return false;
+  return rows_of(a, b, end, len, p, lo, hi, h, is_v, g);
 }
 
 template <int KM, int NH>
@@ -549,8 +583,8 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a) {
   else store_page<KM, NH, kBoth>(a.r, g, a.dh, tops);
 }
 
-// Long pages, in three launches: the exponents that `a.parts` blocks per page and head need
-// for `a.part` tokens each (and the queries), the page's exponent from them, the codes.
+// Long pages, in three launches: the exponents that a block per part and head finds its rows to
+// need (and the queries), the page's exponent from them, the codes.
 template <int KM, int NH, int PHASE>
 __global__ __launch_bounds__(kThreads) void append8_part_kernel(AppendArgs a) {
   __shared__ f32x2 cs[kTok][kMaxPairs];
@@ -561,15 +595,9 @@ __global__ __launch_bounds__(kThreads) void append8_part_kernel(AppendArgs a) {
     append_rows(a, blockIdx.x % a.q_blocks_x, blockIdx.x / a.q_blocks_x, 2 * a.H, cs, index, slot, mine);
     return;
   }
-  const int x = blockIdx.x - nq, unit = x / a.parts, off = (x - unit * a.parts) * a.part;
   PageRows g;
   bool is_v;
-  if (!page_rows(a, unit, NH, g, is_v) || off >= g.n) return;
-  g.src += off * g.ss;
-  g.had += off;
-  g.row0 += off;
-  g.index0 += off;
-  g.n = min(g.n - off, a.part);
+  if (!part_rows(a, blockIdx.x - nq, NH, g, is_v)) return;
   if (is_v) store_page<0, 1, PHASE>(a.r, g, a.dh, tops);
   else store_page<KM, NH, PHASE>(a.r, g, a.dh, tops);
 }
@@ -579,9 +607,10 @@ __global__ __launch_bounds__(kThreads) void append8_exponent_kernel(AppendArgs a
   if (!page_rows(a, blockIdx.x, 1, g, is_v)) return;
   const int old = min((int)*g.exponent, 247) - 127;
   __syncthreads();                               // (every thread has read it)
-  int need = 0;
+  int need = g.page[g.had * g.cs];               // at the parts' first rows
 #pragma unroll 8
-  for (int off = 0; off < g.n; off += a.part) need = max(need, (int)g.page[(g.had + off) * g.cs]);
+  for (int row = ((g.had >> a.part_log2) + 1) << a.part_log2; row < g.had + g.n; row += 1 << a.part_log2)
+    need = max(need, (int)g.page[row * g.cs]);
   const int e = g.had > 0 ? max(old, need - 127) : need - 127;
   if (threadIdx.x == 0) *g.exponent = (uint8_t)(e + 127);
   round_again(g, 0, g.had, e - old, a.dh);
@@ -654,12 +683,13 @@ Rope make_rope(const cast_rope_params_t* p, const int32_t* pos, int transpose) {
   return r;
 }
 
+// `pages`, `parts`: how many of them the call can meet
 template <int KM, int NH>
-void launch_append8_parts(const AppendArgs& a, long long groups, hipStream_t stream) {
-  const unsigned nq = a.q_blocks_x * a.q_shares, units = (unsigned)(groups * (a.H + a.H / NH));
-  hipLaunchKernelGGL((append8_part_kernel<KM, NH, kFind>), dim3(nq + units * a.parts), dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL(append8_exponent_kernel, dim3((unsigned)groups * 2 * a.H), dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL((append8_part_kernel<KM, NH, kStore>), dim3(units * a.parts), dim3(kThreads), 0, stream, a);
+void launch_append8_parts(const AppendArgs& a, long long pages, long long parts, hipStream_t stream) {
+  const unsigned nq = a.q_blocks_x * a.q_shares, units = (unsigned)(parts * (a.H + a.H / NH));
+  hipLaunchKernelGGL((append8_part_kernel<KM, NH, kFind>), dim3(nq + units), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(append8_exponent_kernel, dim3((unsigned)pages * 2 * a.H), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((append8_part_kernel<KM, NH, kStore>), dim3(units), dim3(kThreads), 0, stream, a);
 }
 
 // heads per block: all of them once there are blocks for every compute unit several
@@ -733,30 +763,35 @@ cast_status_t launch_kv_append(const cast_kv_cache_t& c, const cast_kv_seqs_t& s
       a.q_blocks_x = bx;
       a.q_shares = (a.Hq + a.heads - 1) / a.heads;
     }
-    // every group of the call holds a token, or is a sequence's first or last page
-    const long long groups = (long long)s.n_tok / c.page + 2ll * s.n_seq;
-    // The rows of `part` tokens stay in a block's registers.  Where sequences bring many more
+    // every page counted holds a token, or is a sequence's first or last (see page_rows, part_rows)
+    const long long pages = (long long)s.n_tok / c.page + 2ll * s.n_seq;
+    // The rows of a part stay in a block's registers.  Where sequences bring many more
     // to longer pages, several blocks share a page and head, at the price of two more launches:
     // a frame of 1560 tokens and 12 heads that is a page 17 us, 97 with one block each; 4 x
     // 6240 tokens in such pages 100 and 134; but 2 x 300 in pages of 100 13.5 and 11.
     // Two heads of K to a block where that leaves a thousand: 15000 tokens of 8 heads in
     // pages of 64 29 us and 25.5; but 8 x 512 tokens 10.8 and 11.4, 2 x 300 in pages of 100 11
     // and 13.
-    a.part = kKeep * kThreads * 16 / c.dh;
-    a.parts = c.page > 4 * a.part && s.n_tok / s.n_seq > 2 * a.part ? (c.page + a.part - 1) / a.part : 1;
+    const int part = kKeep * kThreads * 16 / c.dh;
+    a.part_log2 = c.dh == 32 ? 8 : c.dh == 64 ? 7 : 6;
+    a.page_parts = fast_div((c.page + part - 1) / part);
+    const long long parts = (long long)s.n_tok / part + s.n_tok / c.page + 4ll * s.n_seq;
     const int mode = a.r.rot == 0 ? 0 : a.r.inter ? 2 : a.r.rot % 16 == 0 ? 1 : 3;
-    const int nh = (mode == 1 || mode == 2) && c.H % 2 == 0 && groups * a.parts * c.H >= 1024 ? 2 : 1;
-    const long long units = groups * (c.H + c.H / nh), blocks = (long long)a.q_blocks_x * a.q_shares + units * a.parts;
-    if (blocks >= (1ll << 24)) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
-    if (a.parts > 1) {
-      if (mode == 0) launch_append8_parts<0, 1>(a, groups, stream);
-      else if (mode == 1 && nh == 2) launch_append8_parts<1, 2>(a, groups, stream);
-      else if (mode == 1) launch_append8_parts<1, 1>(a, groups, stream);
-      else if (mode == 2 && nh == 2) launch_append8_parts<2, 2>(a, groups, stream);
-      else if (mode == 2) launch_append8_parts<2, 1>(a, groups, stream);
-      else launch_append8_parts<3, 1>(a, groups, stream);
+    const long long nq = (long long)a.q_blocks_x * a.q_shares, most = 1ll << 24;
+    auto heads_of = [&](long long n) { return (mode == 1 || mode == 2) && c.H % 2 == 0 && n * c.H >= 1024 ? 2 : 1; };
+    int nh = heads_of(parts);
+    if (c.page > 4 * part && s.n_tok / s.n_seq > 2 * part && nq + parts * (c.H + c.H / nh) < most) {
+      if (mode == 0) launch_append8_parts<0, 1>(a, pages, parts, stream);
+      else if (mode == 1 && nh == 2) launch_append8_parts<1, 2>(a, pages, parts, stream);
+      else if (mode == 1) launch_append8_parts<1, 1>(a, pages, parts, stream);
+      else if (mode == 2 && nh == 2) launch_append8_parts<2, 2>(a, pages, parts, stream);
+      else if (mode == 2) launch_append8_parts<2, 1>(a, pages, parts, stream);
+      else launch_append8_parts<3, 1>(a, pages, parts, stream);
       return check_launch("kv_append");
     }
+    nh = heads_of(pages);
+    const long long blocks = nq + pages * (c.H + c.H / nh);
+    if (blocks >= most) return fail(CAST_ERR_UNSUPPORTED, "kv_append: %lld workgroups are too many", blocks);
     const dim3 grid((unsigned)blocks);
     if (mode == 0) hipLaunchKernelGGL((append8_kernel<0, 1>), grid, dim3(kThreads), 0, stream, a);
     else if (mode == 1 && nh == 2) hipLaunchKernelGGL((append8_kernel<1, 2>), grid, dim3(kThreads), 0, stream, a);

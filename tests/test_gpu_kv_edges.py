@@ -4,8 +4,10 @@ import numpy as np
 import pytest
 import torch
 
-from kv_util import Batch, bf16
+from kv_util import Batch, bf16, f64
+from oracle import kv as O
 from test_gpu_kv_attn import MASKS, run
+from test_gpu_kv_cache import make_rope, run_append
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -22,3 +24,62 @@ def test_narrow_heads_up_to_the_last_page(cast_lib, bits, page, causal, window, 
     last = np.argwhere(b.table == b.pages - 1)[0]
     b.table[tuple(last)], b.table[0, 1] = b.table[0, 1], b.pages - 1
     run(cast_lib, b, bf16(rng, b.n, 6, 32, scale=2.0), 0.2, causal, window, sinks, "narrow")
+
+
+# ---------------------------------------------------------------------------
+# append, e4m3: long pages, positions of several axes
+# ---------------------------------------------------------------------------
+
+def check_codes(cast, b, k, v, rot, inter=False, axes=None, pos=None, q=None):
+    """The cache after an append against the reference's.  The kernel's rotated key is off by at most
+    d = (|x| + |y|) 3e-7: cosine and sine by 7.5e-8, and four roundings of 2^-24 (amplitude, product,
+    sum, and the angle's fp64 ones, which are far below).  So its exponents and codes lie between
+    those of key - d and key + d; values, and rows that were there, equal the reference's."""
+    r, turns, axis = make_rope(cast, rot, axes=axes, interleaved=inter) if rot else (None, None, None)
+    ref, kr = run_append(cast, b, k, v, r, turns, axis, inter, 1.0, pos, q)
+    d = np.zeros_like(kr)
+    x = np.abs(f64(k))
+    for j in range(rot // 2):
+        c0, c1 = (2 * j, 2 * j + 1) if inter else (j, j + rot // 2)
+        d[..., c0] = d[..., c1] = 3e-7 * (x[..., c0] + x[..., c1])
+    lo, hi = b.host(), b.host()
+    O.append(lo, b.cu, b.lens, b.table, kr - d, f64(v))
+    O.append(hi, b.cu, b.lens, b.table, kr + d, f64(v))
+    assert np.array_equal(b.dve.cpu().numpy(), ref["v_exp"]) and np.array_equal(b.dv.cpu().numpy(), ref["v"])
+    exps, codes = b.dke.cpu().numpy(), b.dk.cpu().numpy()
+    least, most = (f(lo["k_exp"], hi["k_exp"]) for f in (np.minimum, np.maximum))
+    assert np.all((least <= exps) & (exps <= most))
+    one = (least == most)[:, None, :, None]                  # else the codes have no common scale
+    assert one.mean() > 0.9
+    got = O.E4M3[codes]
+    inside = (O.E4M3[lo["k"]] <= got) & (got <= O.E4M3[hi["k"]])
+    assert np.all(inside | ~one), np.argwhere(~(inside | ~one))[:5]
+
+
+LONG = [(128, 20, 300, [200, 150, 1, 300, 0, 250, 140, 180], [500, 150, 9, 300, 7, 256, 900, 301]),
+        (64, 40, 700, [400, 300, 200, 350], [800, 300, 1500, 701]),
+        (32, 76, 1100, [700, 600], [1500, 600]),
+        (128, 3, 6000, [200, 140, 150], [6100, 140, 210])]
+
+
+@pytest.mark.parametrize("dh,H,page,new,lens", LONG)
+@pytest.mark.parametrize("layout", ["half", "interleaved", "any", "none"])
+def test_append_e4m3_parts_of_long_pages(cast_lib, dh, H, page, new, lens, layout):
+    """Pages that several blocks share, begun and continued, the same call's queries rotated: one and
+    two heads of K to a block; calls that fill a small part of their pages."""
+    rng = np.random.default_rng(page)
+    b = Batch(rng, new, lens, page, H, dh, 8, spare=3)
+    size = torch.from_numpy((2.0 ** rng.integers(-6, 5, (b.n, 1, 1))).astype(np.float32))
+    k, v = ((bf16(rng, b.n, H, dh).float() * size).to(torch.bfloat16) for _ in range(2))
+    rot, inter = {"half": (dh, False), "interleaved": (dh // 2, True), "any": (22, False), "none": (0, False)}[layout]
+    check_codes(cast_lib, b, k, v, rot, inter, q=bf16(rng, b.n, H, dh) if rot else None)
+
+
+@pytest.mark.parametrize("page,new,lens", [(16, [30, 1, 7], [40, 1, 100]), (300, [200, 150], [430, 150])])
+@pytest.mark.parametrize("rot,inter,axes", [(64, False, None), (128, True, [44, 42, 42]), (96, False, [32, 32, 32]), (60, False, [20, 40])])
+def test_append_e4m3_positions(cast_lib, page, new, lens, rot, inter, axes):
+    """Positions that the call gives, of one axis and of several."""
+    rng = np.random.default_rng(rot)
+    b = Batch(rng, new, lens, page, 4, 128, 8, spare=1)
+    pos = rng.integers(0, 5000, (b.n, len(axes or [1]))).astype(np.int32)
+    check_codes(cast_lib, b, bf16(rng, b.n, 4, 128), bf16(rng, b.n, 4, 128), rot, inter, axes, pos, bf16(rng, b.n, 8, 128))
