@@ -4,7 +4,9 @@ Argument marshalling only: every step of routing, anchor attention and PAR runs 
 the library's HIP kernels.  Tensors are torch device tensors (torch supplies the
 memory and the current HIP stream); the functions carry the C ABI names and
 arguments of include/cast.h, plus small conveniences that allocate outputs and
-workspaces with torch.
+workspaces with torch.  A call given `stream` does all of it as under
+torch.cuda.stream(stream): inputs have to be ready there, and what it returns
+belongs to that stream's memory.
 
 There is no fallback: if libcast.so is missing or fails to load, every call
 raises.
@@ -194,14 +196,25 @@ def _stream(stream):
     return stream.cuda_stream
 
 
-def _ws(nbytes: int, device, workspace):
+def _new(stream, make, *args, **kw):
+    """make(...), with what it allocates (and the kernels that fill it) belonging to `stream`, where the
+    call will use it.  Memory of the current stream would be handed out again there as soon as the
+    call returns, or still be in use there by what had it before, with nothing to order the two."""
+    if stream is None:
+        return make(*args, **kw)
+    import torch
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
+def _ws(nbytes: int, device, workspace, stream=None):
     import torch
     if nbytes == 0:
         return None, 0
     if workspace is not None:
         return workspace, workspace.numel() * workspace.element_size()
     # torch's caching allocator returns >= 512-byte aligned blocks
-    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+    return _new(stream, torch.empty, nbytes, dtype=torch.uint8, device=device), nbytes
 
 
 # ---------------------------------------------------------------------------
@@ -238,10 +251,10 @@ def cast_route_kv(q, k_hist, topk: int, scale: float = 1.0, scores_out=None, idx
     M, Bv = k_hist.shape[0], k_hist.shape[1]
     k_eff_guess = min(topk, M)
     if idx_out is None and M > 0:
-        idx_out = torch.empty((n_a, H, k_eff_guess), dtype=torch.int32, device=q.device)
+        idx_out = _new(stream, torch.empty, (n_a, H, k_eff_guess), dtype=torch.int32, device=q.device)
     if scores_out is None and want_scores and M > 0:
-        scores_out = torch.empty((n_a, H, M), dtype=torch.float32, device=q.device)
-    ws, wsb = _ws(lib.cast_route_kv_workspace_bytes(n_a, S, H, dh, M, Bv), q.device, workspace)
+        scores_out = _new(stream, torch.empty, (n_a, H, M), dtype=torch.float32, device=q.device)
+    ws, wsb = _ws(lib.cast_route_kv_workspace_bytes(n_a, S, H, dh, M, Bv), q.device, workspace, stream)
     k_eff = ctypes.c_int(-1)
     _check(lib.cast_route_kv(_ptr(q), _ptr(k_hist), n_a, S, H, dh, M, Bv, topk, scale,
                              _ptr(scores_out), _ptr(idx_out), ctypes.byref(k_eff), _ptr(ws), wsb,
@@ -267,7 +280,7 @@ def cast_wo_gram(w_o, H: int, dh: int, gram_out=None, stream=None):
     lib = load()
     D = w_o.shape[0]
     if gram_out is None:
-        gram_out = torch.empty((H, dh, dh), dtype=torch.float32, device=w_o.device)
+        gram_out = _new(stream, torch.empty, (H, dh, dh), dtype=torch.float32, device=w_o.device)
     _check(lib.cast_wo_gram(_ptr(w_o), D, H, dh, _ptr(gram_out), _stream(stream)))
     return gram_out
 
@@ -286,12 +299,12 @@ def cast_route_coupled(q, k_hist, v_hist, gram, anchors, n_frames: int, topk: in
     n_a, S, H, dh = q.shape
     M, Bv = k_hist.shape[0], k_hist.shape[1]
     if idx_out is None and M > 0:
-        idx_out = torch.empty((n_a, H, min(topk, M)), dtype=torch.int32, device=q.device)
+        idx_out = _new(stream, torch.empty, (n_a, H, min(topk, M)), dtype=torch.int32, device=q.device)
     if u_out is None and want_u and M > 0:
-        u_out = torch.empty((n_a, H, M), dtype=torch.float32, device=q.device)
+        u_out = _new(stream, torch.empty, (n_a, H, M), dtype=torch.float32, device=q.device)
     anc = [int(a) for a in anchors]
     arr = (ctypes.c_int * max(len(anc), 1))(*anc)
-    ws, wsb = _ws(lib.cast_route_coupled_workspace_bytes(n_a, S, H, dh, M, Bv), q.device, workspace)
+    ws, wsb = _ws(lib.cast_route_coupled_workspace_bytes(n_a, S, H, dh, M, Bv), q.device, workspace, stream)
     k_eff = ctypes.c_int(-1)
     _check(lib.cast_route_coupled(_ptr(q), _ptr(k_hist), _ptr(v_hist), _ptr(gram), arr, n_a,
                                   n_frames, S, H, dh, M, Bv, topk, scale, ctypes.byref(params),
@@ -331,11 +344,11 @@ def cast_frame_select(delta_cam, delta_act, anchors_prev, k_f: int, ages,
     else:
         n_cur, S, D, dtype, device = int(n_cur if n_cur is not None else ages.shape[0]), 1, 1, 0, ages.device
     if anchors_out is None:
-        anchors_out = torch.empty(k_f, dtype=torch.int32, device=device)
+        anchors_out = _new(stream, torch.empty, k_f, dtype=torch.int32, device=device)
     anc = [int(a) for a in anchors_prev]
     arr = (ctypes.c_int * max(len(anc), 1))(*anc)
     nb = lib.cast_frame_select_workspace_bytes(n_cur, S, D) if given else 0
-    ws, wsb = _ws(nb, device, workspace)
+    ws, wsb = _ws(nb, device, workspace, stream)
     _check(lib.cast_frame_select(_ptr(delta_cam), _ptr(delta_act), dtype, n_cur, S, D, arr,
                                  len(anc), k_f, ctypes.byref(params), _ptr(ages), _ptr(r_out),
                                  _ptr(score_out), _ptr(anchors_out), _ptr(ws), wsb,
@@ -371,15 +384,15 @@ def cast_spectral_diagnostics(ref, approx, anchors, params: DiagParams | None = 
         params = cast_diag_params_default()
     n_frames, Hg, Wg, D = ref.shape
     dev = ref.device
-    nrmse = torch.zeros(n_frames, dtype=torch.float32, device=dev)
-    bands = torch.zeros((n_frames, params.n_bands), dtype=torch.float32, device=dev)
-    perr = torch.zeros(n_frames, dtype=torch.float32, device=dev) if theta is not None else None
-    rp = torch.zeros_like(ref) if want_corrections else None
-    rm = torch.zeros_like(ref) if want_corrections else None
+    nrmse = _new(stream, torch.zeros, n_frames, dtype=torch.float32, device=dev)
+    bands = _new(stream, torch.zeros, (n_frames, params.n_bands), dtype=torch.float32, device=dev)
+    perr = _new(stream, torch.zeros, n_frames, dtype=torch.float32, device=dev) if theta is not None else None
+    rp = _new(stream, torch.zeros_like, ref) if want_corrections else None
+    rm = _new(stream, torch.zeros_like, ref) if want_corrections else None
     anc = [int(a) for a in anchors]
     arr = (ctypes.c_int * max(len(anc), 1))(*anc)
     nb = lib.cast_spectral_diagnostics_workspace_bytes(n_frames, Hg, Wg, D, ctypes.byref(params))
-    ws, wsb = _ws(nb, dev, workspace)
+    ws, wsb = _ws(nb, dev, workspace, stream)
     _check(lib.cast_spectral_diagnostics(_ptr(ref), _ptr(approx), _ptr(theta), arr, len(anc),
                                          n_frames, Hg, Wg, D, ctypes.byref(params), _ptr(nrmse),
                                          _ptr(bands), _ptr(perr), _ptr(rp), _ptr(rm), _ptr(ws), wsb,
@@ -399,8 +412,8 @@ def cast_phase_progress(ref, anchors, params: DiagParams | None = None, p_out=No
     n_frames, Hg, Wg, D = ref.shape
     nt = -(-Hg // params.tile_h) * -(-Wg // params.tile_w)
     if p_out is None:
-        p_out = torch.full((n_frames, nt, params.tile_h * (params.tile_w // 2 + 1), D), float("nan"),
-                           dtype=torch.float32, device=ref.device)
+        p_out = _new(stream, torch.full, (n_frames, nt, params.tile_h * (params.tile_w // 2 + 1), D),
+                     float("nan"), dtype=torch.float32, device=ref.device)
     anc = [int(a) for a in anchors]
     arr = (ctypes.c_int * max(len(anc), 1))(*anc)
     _check(lib.cast_phase_progress(_ptr(ref), arr, len(anc), n_frames, Hg, Wg, D,
@@ -424,13 +437,13 @@ def cast_anchor_attn(q, k_hist, v_hist, idx, k_eff: int, scale: float, k_cur=Non
     M, Bv = k_hist.shape[0], k_hist.shape[1]
     n0 = 0 if k_cur is None else k_cur.shape[0]
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, torch.empty_like, q)
     if lse_out is None and want_lse:
-        lse_out = torch.empty((n_a, H, S), dtype=torch.float32, device=q.device)
+        lse_out = _new(stream, torch.empty, (n_a, H, S), dtype=torch.float32, device=q.device)
     ws, wsb = None, 0
     if split:
         ws, wsb = _ws(lib.cast_anchor_attn_workspace_bytes(n_a, S, H, dh, k_eff, n0, Bv), q.device,
-                      workspace)
+                      workspace, stream)
     _check(lib.cast_anchor_attn(_ptr(q), _ptr(k_hist), _ptr(v_hist), _ptr(idx), k_eff,
                                 _ptr(k_cur), _ptr(v_cur), n0, n_a, S, H, dh, M, Bv, scale,
                                 _ptr(out), _ptr(lse_out), _ptr(ws), wsb, _stream(stream)))
@@ -451,9 +464,9 @@ def cast_par_reconstruct(resid, anchors, params: ParParams | None = None, out=No
     anc = [int(a) for a in anchors]
     arr = (ctypes.c_int * max(len(anc), 1))(*anc)
     if out is None:
-        out = torch.zeros_like(resid)
+        out = _new(stream, torch.zeros_like, resid)
     nbytes = lib.cast_par_workspace_bytes(n_frames, len(anc), Hg, Wg, D, ctypes.byref(params))
-    ws, wsb = _ws(nbytes, resid.device, workspace)
+    ws, wsb = _ws(nbytes, resid.device, workspace, stream)
     _check(lib.cast_par_reconstruct(_ptr(resid), arr, len(anc), n_frames, Hg, Wg, D,
                                     ctypes.byref(params), _ptr(out), _ptr(theta_out),
                                     _ptr(gate_out), _ptr(conf_out), _ptr(ws), wsb,
@@ -538,6 +551,8 @@ def _on(device, stream):
         _bad(f"tensors must be on a GPU, got {device}")
     if index != _torch.cuda.current_device():
         _bad(f"tensors are on {device}, the current device is cuda:{_torch.cuda.current_device()}")
+    if stream is not None and stream.device_index != index:
+        _bad(f"tensors are on {device}, the stream on cuda:{stream.device_index}")
     return _torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
 
 
@@ -613,7 +628,7 @@ def cast_rope(x, pos, rope: RopeParams, transpose: bool = False, out=None, strea
         _bad(f"x must be [n, H, dh], got {list(shape)}")
     n, H, dh = shape
     if out is None:
-        out = _torch.empty_like(x, memory_format=_torch.contiguous_format)
+        out = _new(stream, _torch.empty_like, x, memory_format=_torch.contiguous_format)
         os_ = (H * dh, dh, 1)
     else:
         if out.dtype != dtype or out.device != device or out.shape != shape:
@@ -718,7 +733,7 @@ def cast_kv_append(cache: KvCache, seqs: KvSeqs, k, v, rope: RopeParams | None =
         hq = q.shape[1] if q.dim() == 3 else 0
         qs = _rows("q", q, hq, dh, n, dev)
         if q_out is None:
-            q_out = _torch.empty_like(q, memory_format=_torch.contiguous_format)
+            q_out = _new(stream, _torch.empty_like, q, memory_format=_torch.contiguous_format)
         else:
             _same("q_out", q_out, q, _torch.bfloat16)
         qp, op = q.data_ptr(), q_out.data_ptr()
@@ -753,9 +768,9 @@ def cast_kv_read(cache: KvCache, pages, k_out=None, v_out=None, want_k: bool = T
             if t.shape != shape:
                 _bad(f"{name} must be {list(shape)}, got {list(t.shape)}")
     if k_out is None and want_k:
-        k_out = _torch.empty(shape, dtype=_torch.bfloat16, device=dev)
+        k_out = _new(stream, _torch.empty, shape, dtype=_torch.bfloat16, device=dev)
     if v_out is None and want_v:
-        v_out = _torch.empty(shape, dtype=_torch.bfloat16, device=dev)
+        v_out = _new(stream, _torch.empty, shape, dtype=_torch.bfloat16, device=dev)
     st = lib.cast_kv_read(cache.ref, pages.data_ptr(), m, _ptr(k_out), _ptr(v_out), _on(dev, stream))
     if st:
         _check(st)
@@ -791,7 +806,7 @@ def cast_kv_attn(q, cache: KvCache, seqs: KvSeqs, scale: float, causal: bool = T
         _bad(f"the sequences are on {seqs.device}, the cache on {dev}")
     qs = _rows("q", q, hq, cache.dh, n, dev)
     if out is None:
-        out = _torch.empty_like(q, memory_format=_torch.contiguous_format)
+        out = _new(stream, _torch.empty_like, q, memory_format=_torch.contiguous_format)
     else:
         _same("out", out, q, _torch.bfloat16)
     lp = None
@@ -801,7 +816,7 @@ def cast_kv_attn(q, cache: KvCache, seqs: KvSeqs, scale: float, causal: bool = T
             _bad(f"lse_out must be {[n, hq]}, got {list(lse_out.shape)}")
         lp = lse_out.data_ptr()
     elif want_lse:
-        lse_out = _torch.empty((n, hq), dtype=_torch.float32, device=dev)
+        lse_out = _new(stream, _torch.empty, (n, hq), dtype=_torch.float32, device=dev)
         lp = lse_out.data_ptr()
     top, sref, causal = _max_len(cache, seqs, max_len), seqs.ref(n), 1 if causal else 0
     strm = _on(dev, stream)
@@ -814,7 +829,7 @@ def cast_kv_attn(q, cache: KvCache, seqs: KvSeqs, scale: float, causal: bool = T
         else:
             wsb = lib.cast_kv_attn_workspace_bytes(cache.ref, sref, hq, top, causal, window, sinks)
             if wsb:
-                workspace = _torch.empty(wsb, dtype=_torch.uint8, device=dev)
+                workspace = _new(stream, _torch.empty, wsb, dtype=_torch.uint8, device=dev)
                 ws = workspace.data_ptr()
     st = lib.cast_kv_attn(q.data_ptr(), qs, hq, cache.ref, sref, top, causal, window, sinks, scale, out.data_ptr(), lp,
                           ws, wsb, strm)

@@ -83,3 +83,51 @@ def test_append_e4m3_positions(cast_lib, page, new, lens, rot, inter, axes):
     b = Batch(rng, new, lens, page, 4, 128, 8, spare=1)
     pos = rng.integers(0, 5000, (b.n, len(axes or [1]))).astype(np.int32)
     check_codes(cast_lib, b, bf16(rng, b.n, 4, 128), bf16(rng, b.n, 4, 128), rot, inter, axes, pos, bf16(rng, b.n, 8, 128))
+
+
+# ---------------------------------------------------------------------------
+# other streams
+# ---------------------------------------------------------------------------
+
+def test_calls_on_two_streams_at_once(cast_lib):
+    """Calls that cut long ranges, on two streams, with workspaces and outputs made in the call, while
+    the current stream allocates: each gives what it gives alone."""
+    rng = np.random.default_rng(60)
+    sides = []
+    for new, lens in (([1] * 4, [9000, 300, 7000, 4000]), ([40, 60], [9000, 5000])):
+        b = Batch(rng, new, lens, 16, 2, 64, 16)
+        cache, seqs = b.device(cast_lib)
+        q = bf16(rng, b.n, 8, 64).to(DEV)
+        assert cast_lib.cast_kv_attn_workspace_bytes(q, cache, seqs) > 0
+        sides.append((q, cache, seqs, cast_lib.cast_kv_attn(q, cache, seqs, 0.125, want_lse=True)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for i in range(40):
+        q, cache, seqs, _ = sides[i % 2]
+        got.append((i % 2, cast_lib.cast_kv_attn(q, cache, seqs, 0.125, want_lse=True, stream=streams[(i // 2) % 2])))
+        torch.full((1 << 20,), float("nan"), device=DEV)
+    torch.cuda.synchronize()
+    for i, (out, lse) in got:
+        assert torch.equal(out, sides[i][3][0]) and torch.equal(lse, sides[i][3][1])
+
+
+def test_outputs_are_not_memory_that_the_current_stream_still_uses(cast_lib):
+    """Memory that was freed with work on the current stream pending does not become the output of a
+    call on another stream."""
+    rope = cast_lib.cast_rope_params_init(64)
+    x = torch.randn((4096, 8, 64), device=DEV).bfloat16()
+    pos = torch.arange(4096, dtype=torch.int32, device=DEV)
+    want = cast_lib.cast_rope(x, pos, rope)
+    busy = torch.randn((4096, 4096), device=DEV)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(5):
+        old = torch.empty_like(x)
+        for _ in range(4):
+            busy = torch.mm(busy, busy).clamp_(-1.0, 1.0)    # some milliseconds
+        old.fill_(7.0)
+        del old
+        got = cast_lib.cast_rope(x, pos, rope, stream=s)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)

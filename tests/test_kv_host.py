@@ -1,10 +1,10 @@
 """Host side of the cached-history calls: its C++ functions that are not part of the C ABI,
 sizes that have to pass or to be refused, and what the binding does around a call."""
-import ctypes
 import os
+from types import SimpleNamespace
 
-import numpy as np
 import pytest
+import torch
 
 import paper_2609_34144_amd as cast
 from test_abi import _HAS_GPU
@@ -43,3 +43,89 @@ def test_pages_far_longer_than_the_call_are_taken(lib):
     s = seqs(n_seq=64, n_tok=12800, max_pages=2)
     for r in (False, rope(rot_dim=128), rope(rot_dim=30)):
         assert append(lib, c, s, r, ks=1024, vs=1024) == HIP, lib.cast_last_error_detail()
+
+
+# ---------------------------------------------------------------------------
+# the binding: what it allocates belongs to the stream of the call
+# ---------------------------------------------------------------------------
+
+class _AnyCall:
+    """A library whose calls succeed without doing anything and want 256 bytes of workspace."""
+
+    def __getattr__(self, name):
+        return lambda *a: 256 if name.endswith("bytes") else 0
+
+
+def _calls():
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    z = lambda *s, d=bf: torch.zeros(s, dtype=d)  # noqa: E731
+    q, kv, frames = z(1, 8, 2, 64), z(3, 8, 2, 64), z(4, 8, 8, 2, d=f32)
+    cache, seqs = cast.KvCache(z(4, 16, 2, 64), z(4, 16, 2, 64)), cast.KvSeqs(z(3, d=i32), z(2, d=i32), z(2, 4, d=i32))
+    rope = cast.RopeParams(z(32, d=torch.float64), z(32, d=torch.uint8))
+    k, qn, pos = z(5, 2, 64), z(5, 4, 64), z(5, d=i32)
+    dp = cast.DiagParams(tile_h=8, tile_w=8, n_bands=2)
+    return {
+        "route_kv": (3, lambda s: cast.cast_route_kv(q, kv, 2, want_scores=True, stream=s)),
+        "wo_gram": (1, lambda s: cast.cast_wo_gram(z(128, 128), 2, 64, stream=s)),
+        "route_coupled": (3, lambda s: cast.cast_route_coupled(q, kv, kv, z(2, 64, 64, d=f32), [0], 4, 2, 1.0,
+                                                               cast.CoupledParams(), want_u=True, stream=s)),
+        "frame_select": (2, lambda s: cast.cast_frame_select(z(4, 8, 2), None, [0, 3], 2, z(4, d=i32), cast.SelectParams(), stream=s)),
+        "spectral_diagnostics": (6, lambda s: cast.cast_spectral_diagnostics(frames, frames, [0, 3], dp, theta=frames,
+                                                                             want_corrections=True, stream=s)),
+        "phase_progress": (1, lambda s: cast.cast_phase_progress(frames, [0, 3], dp, stream=s)),
+        "anchor_attn": (3, lambda s: cast.cast_anchor_attn(q, kv, kv, z(1, 2, 2, d=i32), 2, 1.0, want_lse=True, stream=s)),
+        "par_reconstruct": (2, lambda s: cast.cast_par_reconstruct(frames, [0, 3], cast.ParParams(), stream=s)),
+        "rope": (1, lambda s: cast.cast_rope(k, pos, rope, stream=s)),
+        "kv_append": (1, lambda s: cast.cast_kv_append(cache, seqs, k, k, rope, q=qn, stream=s)),
+        "kv_read": (2, lambda s: cast.cast_kv_read(cache, z(2, d=i32), stream=s)),
+        "kv_attn": (3, lambda s: cast.cast_kv_attn(qn, cache, seqs, 0.1, want_lse=True, stream=s)),
+    }
+
+
+@pytest.mark.parametrize("name", ["route_kv", "wo_gram", "route_coupled", "frame_select", "spectral_diagnostics", "phase_progress",
+                                  "anchor_attn", "par_reconstruct", "rope", "kv_append", "kv_read", "kv_attn"])
+def test_allocations_belong_to_the_stream_of_the_call(lib, monkeypatch, name):
+    """Outputs and workspaces of a call on another stream than the current one are that stream's:
+    else the caching allocator would give a workspace to the current stream's next allocation while
+    the call still runs (two calls on two streams would share one), or an output's memory would
+    still be in use there."""
+    count, call = _calls()[name]
+    current, made = [], []
+
+    class Under:
+        def __init__(self, s):
+            self.s = s
+
+        def __enter__(self):
+            current.append(self.s)
+
+        def __exit__(self, *a):
+            current.pop()
+
+    def watch(f):
+        def make(*a, **kw):
+            made.append(current[-1] if current else None)
+            return f(*a, **kw)
+        return make
+
+    stream = SimpleNamespace(cuda_stream=0x40, device_index=0)
+    monkeypatch.setattr(cast, "_lib", _AnyCall())
+    monkeypatch.setattr(cast, "_on", lambda device, s: 0)
+    monkeypatch.setattr(torch.cuda, "stream", Under)
+    for f in ("empty", "empty_like", "zeros", "zeros_like", "full"):
+        monkeypatch.setattr(torch, f, watch(getattr(torch, f)))
+    call(stream)
+    assert made[-count:] == [stream] * count, made           # (inputs that the call's line makes come first)
+    if name in ("rope", "kv_append", "kv_read", "kv_attn"):
+        call(None)                                           # no stream: the current one, no switch
+        assert made[-count:] == [None] * count
+
+
+def test_a_stream_of_another_device_is_refused(lib, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    gpu = torch.device("cuda", 0)
+    assert cast._on(gpu, SimpleNamespace(cuda_stream=0x40, device_index=0)) == 0x40
+    for device, stream in ((gpu, SimpleNamespace(cuda_stream=0x40, device_index=1)),
+                           (torch.device("cuda", 1), SimpleNamespace(cuda_stream=0x40, device_index=1))):
+        with pytest.raises(cast.CastError):
+            cast._on(device, stream)
