@@ -714,10 +714,10 @@ cast_status_t launch_rope(const void* x, int dtype, int n, int H, int dh, long l
   const Items it = plan_items(r.rot, r.inter, dh, wide);
   const int heads = heads_per_block((n + kTok - 1) / kTok, H, it.per_head);
   constexpr int kMost = 1 << 25;                 // tokens of a launch, whose threads must stay below 2^32
-  for (int at = 0; at < n; at += kMost) {
-    const int m = std::min(n - at, kMost);
+  for (long long at = 0; at < n; at += kMost) {
+    const int m = (int)std::min<long long>(n - at, kMost);
     const dim3 grid((m + kTok - 1) / kTok, (H + heads - 1) / heads);
-    r.pos = pos + (long long)at * r.n_axes;
+    r.pos = pos + at * r.n_axes;
     if (dtype == 0)
       hipLaunchKernelGGL((rope_kernel<float>), grid, dim3(kThreads), 0, stream, static_cast<const float*>(x) + at * xt,
                          xt, xh, static_cast<float*>(out) + at * yt, yt, yh, m, H, heads, r, it);
@@ -821,12 +821,12 @@ cast_status_t launch_kv_read(const cast_kv_cache_t& c, const int32_t* idx, int m
   const unsigned parts = (unsigned)std::min<long long>((a.chunks + 4 * kThreads - 1) / (4 * kThreads), 65535);
   const unsigned z = ko != nullptr && vo != nullptr ? 2 : 1;
   // pages beyond the grid's limit of rows go in further launches
-  for (int at = 0; at < m; at += 65535) {
+  for (long long at = 0; at < m; at += 65535) {
     ReadArgs b = a;
     b.idx = idx + at;
-    if (ko != nullptr) b.ko = a.ko + (long long)at * a.chunks * 8;
-    if (vo != nullptr) b.vo = a.vo + (long long)at * a.chunks * 8;
-    const dim3 grid(parts, (unsigned)std::min(m - at, 65535), z);
+    if (ko != nullptr) b.ko = a.ko + at * a.chunks * 8;
+    if (vo != nullptr) b.vo = a.vo + at * a.chunks * 8;
+    const dim3 grid(parts, (unsigned)std::min(m - at, 65535ll), z);
     if (c.dtype == 2) hipLaunchKernelGGL((read_kernel<true>), grid, dim3(kThreads), 0, stream, b);
     else hipLaunchKernelGGL((read_kernel<false>), grid, dim3(kThreads), 0, stream, b);
   }

@@ -1,6 +1,8 @@
 """Host side of the cached-history calls: its C++ functions that are not part of the C ABI,
 sizes that have to pass or to be refused, and what the binding does around a call."""
 import os
+import subprocess
+import sys
 from types import SimpleNamespace
 
 import pytest
@@ -129,3 +131,16 @@ def test_a_stream_of_another_device_is_refused(lib, monkeypatch):
                            (torch.device("cuda", 1), SimpleNamespace(cuda_stream=0x40, device_index=1))):
         with pytest.raises(cast.CastError):
             cast._on(device, stream)
+
+
+@pytest.mark.parametrize("call", ["r_rope(lib, n=2 ** 31 - 1, H=1, dh=32, xt=32, xh=32, yt=32, yh=32)",
+                                  "read(lib, cache(pages=1, page=1, H=1, dh=32), m=2 ** 31 - 1)"])
+def test_launches_of_the_largest_counts_end(lib, call):
+    """Tokens and pages next to 2^31 go in several launches, whose counter must not wrap."""
+    if _HAS_GPU:
+        pytest.skip("calls with fake pointers run GPU-less only")
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = (f"import sys; sys.path[:0] = [{os.path.dirname(here)!r}, {here!r}]\n"
+            "import paper_2609_34144_amd as cast\nlib = cast.load()\nfrom test_kv_abi import cache, r_rope, read\n"
+            f"sys.exit({call})")
+    assert subprocess.run([sys.executable, "-c", code], timeout=60).returncode == HIP
