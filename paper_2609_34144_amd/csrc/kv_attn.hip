@@ -66,12 +66,19 @@ constexpr int kJoinWays = 8;   // threads that share the pieces of a row, from a
 // s_waitcnt vmcnt(0) that leaves expcnt and lgkmcnt free
 constexpr int kVmcnt0 = 0x0F70;
 // The running maximum moves only when a tile exceeds it by more than this, in log2 units
-// (see softmax): probabilities reach 2^16, where sums of 2^24 keys of values below 2^80 are
-// still far from overflow, and the exponent's argument is off by 2^-21 at most.  With 2^8,
-// keys whose logits spread by 6 moved some wave's maximum in nearly every tile (chunks of
-// 64-wide heads 177 us, so 144; the frame over an 8-bit window 167 and 145).
+// (see softmax).  With 2^8, keys whose logits spread by 6 moved some wave's maximum in nearly
+// every tile (chunks of 64-wide heads 177 us, so 144; the frame over an 8-bit window 167 and 145).
 constexpr float kMaxSlack = 16.0f;
-constexpr float kSumBound = 65536.0f;   // 2^kMaxSlack
+// It is kept this much above the scores', in log2 units: exponentials start at 2^-46 and reach
+// 2^-30 at most, so those of a row of 2^30 keys (the longest) sum to at most one, and their
+// products with the values to at most the largest value, which may be the type's.  (With the
+// maximum at the scores' own, finite values above 2^111 could give infinite rows.)  What falls
+// below 2^-126 is lost, as ever; that is 2^-80 of the largest.  The exponent's argument is off by
+// 2^-19 at most, an exponential by 2^-19 of itself.
+constexpr float kLead = 46.0f;
+constexpr float kSumBound = 0x1p-30f;   // 2^(kMaxSlack - kLead)
+constexpr float kLeadScale = 0x1p46f;   // 2^kLead
+constexpr float kJoinScale = 0x1p-14f;  // of a piece in a sum of up to 2^14 of them
 // "no key seen yet": below every finite scaled score, so the first visible key moves it
 constexpr float kNoMax = -3.0e38f;
 constexpr float kLn2 = 0.69314718055994531f;
@@ -378,7 +385,7 @@ __device__ __forceinline__ void mask_scores(f32x16 (&sn)[NB], int j0, int hf, Ro
 
 // Exponentials of a tile against the running maximum, in place of the scores (a second set
 // would cost the registers of two waves per SIMD at 64-wide heads), packed as P^T operands,
-// and their sum.  A lane's sum of at most 2^16 shows that no score is far above the maximum,
+// and their sum.  A lane's sum of at most kSumBound shows that no score is far above the maximum,
 // which then may stay; else the scores are formed again, the maximum is taken over the tile, moved, and the sums
 // so far scaled down.
 template <int NB, int ND, class S>
@@ -400,7 +407,7 @@ __device__ __forceinline__ void softmax(f32x16 (&sn)[NB], S&& scores, bf16x8 (&p
     float pm = sn[0][0];
 #pragma unroll
     for (int e = 1; e < NB * 16; ++e) pm = fmaxf(pm, sn[e / 16][e % 16]);
-    const float cand = fmaxf(m_run, half_swap_max(pm) * sl2);
+    const float cand = fmaxf(m_run, fmaf(half_swap_max(pm), sl2, kLead));
     const bool up = cand > m_run + kMaxSlack;
     const float m_new = up ? cand : m_run;
     const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -541,7 +548,7 @@ __device__ __forceinline__ void finish(const KvAttnArgs& a, const Unit& un, long
   const float l = l_run + __shfl_xor(l_run, 32);
   const bool some = l != 0.0f;               // true for NaN, too
   const float inv = some ? 1.0f / l : 0.0f;
-  const float l2 = some ? m_run + __log2f(l) : -INFINITY;
+  const float l2 = some ? (m_run - kLead) + __log2f(l * kLeadScale) : -INFINITY;
   const long long at = (long long)un.z * a.s.n_tok * a.Hq + row;
   if (a.target > 0 && un.z == 0 && hf == 0) a.cuts[row] = un.pieces;
   if (un.pieces > 1) {
@@ -1373,7 +1380,7 @@ __global__ __launch_bounds__(kThreads, row_groups(DH)) void kv_rows_kernel(KvAtt
         float pm = sn[0][0];
 #pragma unroll
         for (int e = 1; e < 8 * SUB; ++e) pm = fmaxf(pm, sn[e / 4][e % 4]);
-        const float cand = fmaxf(m_run, quarter_max(pm) * a.sl2);
+        const float cand = fmaxf(m_run, fmaf(quarter_max(pm), a.sl2, kLead));
         const bool up = cand > m_run + kMaxSlack;
         const float m_new = up ? cand : m_run;
         const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -1464,7 +1471,7 @@ __global__ __launch_bounds__(kThreads, row_groups(DH)) void kv_rows_kernel(KvAtt
     }
     const bool some = lt != 0.0f;                    // true for NaN, too
     o *= some ? 1.0f / lt : 0.0f;
-    const float l2 = some ? m + __log2f(lt) : -INFINITY;
+    const float l2 = some ? (m - kLead) + __log2f(lt * kLeadScale) : -INFINITY;
     if (it.pieces > 1) {
       const long long at = ((long long)blockIdx.x * a.wh + hw) * TM + ql;
       *reinterpret_cast<f32x4*>(a.part_o + at * DH + d) = o;
@@ -1522,7 +1529,7 @@ __global__ __launch_bounds__(kThreads) void kv_rows_join_kernel(KvAttnArgs a) {
     const float c = l == m ? 1.0f : __builtin_amdgcn_exp2f(l - m);
     if (l != -INFINITY) {
       w += c;
-      o += c * p;
+      o += (c * kJoinScale) * p;
     }
   }
   part[tid] = o;
@@ -1535,7 +1542,7 @@ __global__ __launch_bounds__(kThreads) void kv_rows_join_kernel(KvAttnArgs a) {
     o += part[k * PER + tid];
   }
   const bool some = w != 0.0f;
-  o *= some ? 1.0f / w : 0.0f;
+  o *= some ? (1.0f / kJoinScale) / w : 0.0f;
   const int rr = t.row0 + ql, tk = rr / a.g;
   const long long row = (long long)(t.beg + tk) * a.Hq + blockIdx.y * a.g + (rr - tk * a.g);
   put4(a, row, DH, d, o);
@@ -1582,7 +1589,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(KvAttnArgs a) {
     const float c = l == m ? 1.0f : __builtin_amdgcn_exp2f(l - m);
     if (l != -INFINITY) {   // else nothing was written
       w += c;
-      o += c * p;
+      o += (c * kJoinScale) * p;
     }
   }
   if constexpr (WAYS > 1) {
@@ -1600,7 +1607,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(KvAttnArgs a) {
   const int tok = (int)(row / a.Hq);
   if (tok < seq_row(a.s, 0) || tok >= seq_row(a.s, a.s.n_seq)) return;   // of no sequence: left alone
   const bool some = w != 0.0f;
-  o *= some ? 1.0f / w : 0.0f;
+  o *= some ? (1.0f / kJoinScale) / w : 0.0f;
   put4(a, row, DH, d, o);
   if (a.lse != nullptr && d == 0) a.lse[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
 }

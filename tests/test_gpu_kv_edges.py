@@ -7,6 +7,7 @@ import torch
 from kv_util import Batch, bf16, f64
 from oracle import kv as O
 from test_gpu_kv_attn import MASKS, run
+from test_gpu_kv_attn_many import run as run_some
 from test_gpu_kv_cache import make_rope, run_append
 
 pytestmark = pytest.mark.gpu
@@ -131,3 +132,51 @@ def test_outputs_are_not_memory_that_the_current_stream_still_uses(cast_lib):
         got = cast_lib.cast_rope(x, pos, rope, stream=s)
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+# ---------------------------------------------------------------------------
+# attention: values up to the type's largest
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("H,dh,new,what", [(2, 64, [1, 2, 9], "rows"), (2, 64, [40, 70, 3], "tiles"), (3, 128, [200, 60, 130], "tiles"),
+                                           (64, 128, [300, 200, 260], "pairs"), (1, 32, [1, 1, 1], "rows in pieces"),
+                                           (2, 128, [60, 20, 40], "tiles in pieces")])
+def test_the_largest_finite_values(cast_lib, bits, H, dh, new, what):
+    """Values up to 2^127 under scores that rise by up to 10 (less than 2^16 in all) over the keys: a
+    row's result is finite, whatever the sums on the way, and as exact as for small values."""
+    rng = np.random.default_rng(61)
+    lens = [700, 300, 520] if "pieces" not in what else [9000, 3000, 7000]
+    b = Batch(rng, new, lens, 16, H, dh, bits, spread=False)
+    # scores: q = 1 in one channel, the key's channel 0 rises with its index
+    q = torch.zeros((b.n, H, dh))
+    q[:, :, 0] = 1.0
+    for s, L in enumerate(lens):
+        t = np.arange(L)
+        at, row = b.table[s, t // 16], t % 16
+        rise = np.floor(10.0 * t / L * 16) / 16
+        b.k[at, row] = 0
+        if bits == 16:
+            b.k[at, row, :, 0] = torch.from_numpy(rise.astype(np.float32)).to(torch.bfloat16)[:, None]
+        else:
+            code = torch.from_numpy(O.e4m3_code(rise))
+            b.k[at, row, :, 0] = code[:, None]
+    if bits == 16:
+        b.v = (b.v.float().clamp(-1.9, 1.9) * 2.0 ** 126).to(torch.bfloat16)
+    else:
+        b.ke.fill_(127)
+        b.v = torch.from_numpy(O.e4m3_code(rng.uniform(-240.0, 240.0, tuple(b.v.shape))))
+        b.ve.fill_(127 + 119)                                # 240 * 2^119 < 2^127
+    for causal, window in ((True, 0), (False, 250)):
+        run_some(cast_lib, b, q.to(torch.bfloat16), 1.0, causal, window, 3, what)
+
+
+def test_uniform_scores_over_the_largest_values(cast_lib):
+    """Keys of one score whose values are all 2^127: their mean is that, their sum is not finite."""
+    rng = np.random.default_rng(62)
+    for new, dh, H in ((1, 64, 2), (50, 64, 2), (300, 128, 64)):
+        b = Batch(rng, [new], [2000], 16, H, dh, 16)
+        b.k.zero_()
+        b.v.fill_(2.0 ** 127)
+        out, _ = run_some(cast_lib, b, bf16(rng, b.n, H, dh), 0.1, False, what="uniform")
+        assert bool(((out.float() / 2.0 ** 127 - 1.0).abs() <= 2.0 ** -7).all())
