@@ -623,8 +623,8 @@ size_t cast_kv_attn_workspace_bytes(const cast_kv_cache_t* cache, const cast_kv_
  * places, infinities and NaN included, does not reach the row.  fp32 logits, softmax and
  * sums; probabilities are rounded to bf16 for the second product; bf16 output.  No sum exceeds
  * the largest of the values, so finite ones give finite rows (but for the output's own rounding
- * next to the type's largest); a key of less than 2^-80 of the row's largest probability may
- * count as none.
+ * next to the type's largest); a key of less than 2^-80 of the row's largest probability, and a
+ * product of probability and value of less than 2^-80, may count as none.
  *
  * q        bf16 [n_tok, Hq, dh] device; token t at t * q_stride elements (>= Hq * dh, multiple
  *          of 8), heads dense.  Hq a multiple of cache->H.

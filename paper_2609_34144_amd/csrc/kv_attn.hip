@@ -73,8 +73,8 @@ constexpr float kMaxSlack = 16.0f;
 // 2^-30 at most, so those of a row of 2^30 keys (the longest) sum to at most one, and their
 // products with the values to at most the largest value, which may be the type's.  (With the
 // maximum at the scores' own, finite values above 2^111 could give infinite rows.)  What falls
-// below 2^-126 is lost, as ever; that is 2^-80 of the largest.  The exponent's argument is off by
-// 2^-19 at most, an exponential by 2^-19 of itself.
+// below 2^-126 is lost, as ever; that is 2^-80 of the largest exponential, and products below
+// 2^-80 in size.  The exponent's argument is off by 2^-19 at most, an exponential by 2^-19 of itself.
 constexpr float kLead = 46.0f;
 constexpr float kSumBound = 0x1p-30f;   // 2^(kMaxSlack - kLead)
 constexpr float kLeadScale = 0x1p46f;   // 2^kLead
