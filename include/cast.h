@@ -534,7 +534,9 @@ cast_status_t cast_rope(const void* x, int dtype, int n, int H, int dh, long lon
  * exponent byte per (page, head), value = code * 2^(byte - 127).  The scales are powers
  * of two, so every value of an 8-bit cache is a bf16 number exactly.  (cast_kv_append
  * writes bytes 10 .. 247.  Byte 247 belongs to values next to the largest bf16 number,
- * and those that round up from there are infinite.)
+ * and those that round up from there are infinite.  Of bytes that come from elsewhere, 0 to 2
+ * give bf16 subnormals, to which values are rounded; from 247 on values past bf16's range are
+ * infinite; 255 makes all of its page and head NaN.)
  */
 typedef struct {
   void* k;                /* device [pages, page, H, dh] bf16 or uint8 codes            */

@@ -125,7 +125,8 @@ def append(cache, cu, lens, table, k, v):
 
 
 def values(codes, exps):
-    return E4M3[codes] * (2.0 ** (exps.astype(np.float64) - 127.0))[:, None, :, None]
+    scale = np.where(exps == 255, math.nan, 2.0 ** (exps.astype(np.float64) - 127.0))
+    return E4M3[codes] * scale[:, None, :, None]
 
 
 # ---------------------------------------------------------------- attention

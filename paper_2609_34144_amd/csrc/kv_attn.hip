@@ -133,14 +133,9 @@ __device__ __forceinline__ float half_swap_max(float x) {
 __device__ __forceinline__ constexpr int kswz(int r, int cpr) { return (r / (16 / cpr)) & (cpr - 1); }
 __device__ __forceinline__ constexpr int vswz(int r, int cpr) { return ((2 * (r & 3)) ^ (8 * (r & 1))) & (cpr - 1); }
 
-// eight e4m3 codes (two dwords) times 2^(exponent of sc), exact in bf16
 __device__ __forceinline__ u32x4 widen8(uint32_t a, uint32_t b, float sc) {
-  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, sc, false)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, sc, true)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, sc, false)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, sc, true))};
+  return u32x4{widen2<false>(a, sc), widen2<true>(a, sc), widen2<false>(b, sc), widen2<true>(b, sc)};
 }
-__device__ __forceinline__ float byte_scale(int e) { return __uint_as_float((uint32_t)e << 23); }
 
 // ---- the row tile of a workgroup and the key tiles it meets ----------------------------
 struct RowTile {

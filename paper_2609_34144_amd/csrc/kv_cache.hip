@@ -291,7 +291,8 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, f
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
 }
-__device__ __forceinline__ float exp_scale(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// 2^-e for -127 < e <= 128 (below 2^-126 a subnormal)
+__device__ __forceinline__ float inverse_scale(int e) { return __uint_as_float(e < 127 ? (uint32_t)(127 - e) << 23 : 0x00400000u >> (e - 127)); }
 
 // the least e >= -117 with top <= 448 * 2^e (448 = 0.875 * 2^9)
 __device__ __forceinline__ int need_exp(float top) {
@@ -334,7 +335,7 @@ constexpr int kKeep = 2;
 __device__ __forceinline__ void round_again(const PageRows& g, int at, int rows, int up, int dh) {
   if (rows == 0 || up <= 0) return;
   const int ipr = dh >> 4, shift = 31 - __clz(ipr), item = threadIdx.x & (ipr - 1), step = kThreads >> shift;
-  const float down = up < 127 ? exp_scale(-up) : 0.0f;
+  const float down = up < 127 ? inverse_scale(up) : 0.0f;
   for (int t = threadIdx.x >> shift; t < rows; t += step) {
     u32x4* p = reinterpret_cast<u32x4*>(g.page + t * g.cs + at + 16 * item);
     const u32x4 w = *p;
@@ -448,7 +449,7 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
   };
   int old[NH];
 #pragma unroll
-  for (int h = 0; h < NH; ++h) old[h] = min((int)g.exponent[h], 247) - 127;
+  for (int h = 0; h < NH; ++h) old[h] = (int)g.exponent[h] - 127;
   const int batch = kKeep * step;
   float keep[NH][kKeep][16];
 #pragma unroll 1
@@ -488,7 +489,7 @@ __device__ __forceinline__ void store_page(const Rope& r, const PageRows& g, int
         uint8_t* at = g.page + (g.had + t) * g.cs;
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
-          const float inv = exp_scale(-ex[h]);
+          const float inv = inverse_scale(ex[h]);
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const float* y = &keep[h][j][8 * k];
@@ -605,7 +606,7 @@ __global__ __launch_bounds__(kThreads) void append8_exponent_kernel(AppendArgs a
   PageRows g;
   bool is_v;
   if (!page_rows(a, blockIdx.x, 1, g, is_v)) return;
-  const int old = min((int)*g.exponent, 247) - 127;
+  const int old = (int)*g.exponent - 127;
   __syncthreads();                               // (every thread has read it)
   int need = g.page[g.had * g.cs];               // at the parts' first rows
 #pragma unroll 8
@@ -654,15 +655,8 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
     if constexpr (F8) {
       const u32x2 w = *reinterpret_cast<const u32x2*>(src + 8 * c);
       const int at = (int)(c >> a.cph_log2), head = at - div_by(at, a.heads) * a.H;   // at: token and head
-      const float sc = __uint_as_float((uint32_t)ex[head] << 23);
-      u32x4 o;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const f32x2 f = k % 2 == 0 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k >> 1], false)
-                                   : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k >> 1], true);
-        o[k] = pack_bf16(f.x * sc, f.y * sc);
-      }
-      *reinterpret_cast<u32x4*>(out + 8 * c) = o;
+      const float sc = byte_scale(ex[head]);
+      *reinterpret_cast<u32x4*>(out + 8 * c) = u32x4{widen2<false>(w.x, sc), widen2<true>(w.x, sc), widen2<false>(w.y, sc), widen2<true>(w.y, sc)};
     } else {
       *reinterpret_cast<u32x4*>(out + 8 * c) = *reinterpret_cast<const u32x4*>(src + 16 * c);
     }

@@ -52,6 +52,15 @@ __device__ __forceinline__ int find_seq(int n_seq, int x, F&& start) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// Two e4m3 codes, the lower or upper ones of a word, under the scale of an exponent byte, as bf16:
+// code * 2^(byte - 127), exactly where bf16 has that (always from byte 3 to 246), infinite past its
+// range; all NaN for byte 255.
+__device__ __forceinline__ float byte_scale(int e) { return __uint_as_float((uint32_t)e << 23); }
+template <bool HI>
+__device__ __forceinline__ uint32_t widen2(uint32_t codes, float sc) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, sc, HI));
+}
+
 // The rotation as the kernels read it.
 struct Rope {
   const double* turns;

@@ -180,3 +180,67 @@ def test_uniform_scores_over_the_largest_values(cast_lib):
         b.v.fill_(2.0 ** 127)
         out, _ = run_some(cast_lib, b, bf16(rng, b.n, H, dh), 0.1, False, what="uniform")
         assert bool(((out.float() / 2.0 ** 127 - 1.0).abs() <= 2.0 ** -7).all())
+
+
+# ---------------------------------------------------------------------------
+# every exponent byte
+# ---------------------------------------------------------------------------
+
+def all_bytes(cast, page=16, dh=32):
+    """A cache with a page for each exponent byte, in which every code lies; its values as bf16
+    (float64), rounded there once."""
+    codes = torch.arange(page * dh).to(torch.uint8).reshape(1, page, 1, dh).repeat(256, 1, 1, 1)
+    exps = torch.arange(256).to(torch.uint8)[:, None].contiguous()
+    k, ones = torch.zeros_like(codes), torch.full_like(exps, 127)
+    cache = cast.KvCache(k.to(DEV), codes.to(DEV), ones.to(DEV), exps.to(DEV))
+    want = f64(torch.from_numpy(O.values(codes.numpy(), exps.numpy())).float().to(torch.bfloat16))
+    return cache, want
+
+
+def same(got, want):
+    return (got == want) | (np.isnan(got) & np.isnan(want))
+
+
+def test_every_exponent_byte_is_read(cast_lib):
+    cache, want = all_bytes(cast_lib)
+    idx = torch.arange(256, dtype=torch.int32, device=DEV)
+    _, v = cast_lib.cast_kv_read(cache, idx, want_k=False)
+    ok = same(f64(v), want)
+    assert ok.all(), np.argwhere(~ok)[:5]
+    assert np.isnan(f64(v)[255]).all()
+
+
+@pytest.mark.parametrize("rows", ["few", "many"])
+def test_every_exponent_byte_is_attended(cast_lib, rows):
+    """A row that sees one key gives its value, as cast_kv_read does; what lies beside it, infinite or
+    NaN, does not reach the row.  Terms below 2^-80 may be lost."""
+    page, dh = 16, 32
+    cache, want = all_bytes(cast_lib, page, dh)
+    i32 = lambda x: torch.as_tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    if rows == "few":                                        # the last row of each page
+        seqs = cast_lib.KvSeqs(i32(range(257)), i32([page] * 256), i32(range(256))[:, None].contiguous())
+        want = want[:, -1]
+    else:
+        seqs = cast_lib.KvSeqs(i32([0, 256 * page]), i32([256 * page]), i32(range(256))[None].contiguous())
+        want = want.reshape(256 * page, 1, dh)
+    q = torch.ones((len(want), 1, dh), dtype=torch.bfloat16, device=DEV)
+    got = f64(cast_lib.cast_kv_attn(q, cache, seqs, 0.1, True, 1, 0)[0])
+    with np.errstate(invalid="ignore"):
+        ok = same(got, want) | (np.abs(got - want) <= 2.0 ** -80)
+    assert ok.all(), (np.argwhere(~ok)[:5], got[~ok][:5], want[~ok][:5])
+
+
+@pytest.mark.parametrize("size", [2.0 ** 127, 1.0, 2.0 ** -120])
+def test_every_exponent_byte_is_appended_to(cast_lib, size):
+    """Tokens into pages that begin with any exponent: it only grows, earlier codes follow it."""
+    rng = np.random.default_rng(63)
+    b = Batch(rng, [3] * 256, [9] * 256, 16, 2, 32, 8)
+    ex = np.arange(256)
+    b.ke[b.table[:, 0]] = torch.from_numpy(np.stack([ex, ex[::-1]], 1).astype(np.uint8))
+    b.ve[b.table[:, 0]] = torch.from_numpy(np.stack([(ex + 100) % 256, ex], 1).astype(np.uint8))
+    x = torch.from_numpy(rng.uniform(-1.9, 1.9, (b.n, 2, 32)) * size).float().to(torch.bfloat16)
+    ref, _ = run_append(cast_lib, b, x, x)
+    for codes, exps, name in ((b.dk, b.dke, "k"), (b.dv, b.dve, "v")):
+        assert np.array_equal(exps.cpu().numpy(), ref[name + "_exp"])
+        ok = same(O.E4M3[codes.cpu().numpy()], O.E4M3[ref[name]])
+        assert ok.all(), np.argwhere(~ok)[:5]
