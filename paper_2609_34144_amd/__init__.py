@@ -511,6 +511,16 @@ def _bad(msg: str):
     raise CastError(2, msg)                        # CAST_ERR_SHAPE, before the library is asked
 
 
+_INT_MAX = 0x7fffffff             # ctypes takes the low bits of what a C int does not hold
+
+
+def _ints(what: str, *values):
+    """Refuse sizes that a C int does not hold."""
+    for v in values:
+        if not 0 <= v <= _INT_MAX:
+            _bad(f"{what} must be at least 0 and below 2^31, got {', '.join(str(x) for x in values)}")
+
+
 def _want(name: str, t, dtypes, device=None, dense: bool = True):
     """The binding's checks of a tensor the C ABI sees as a bare pointer."""
     if t.dtype not in dtypes:
@@ -564,10 +574,10 @@ def cast_rope_frequencies(axis_dims, base: float = 10000.0, scaling: str = "none
     dims = [int(d) for d in axis_dims]
     if scaling not in ROPE_SCALING:
         _bad(f"scaling must be one of {sorted(ROPE_SCALING)}, got {scaling!r}")
-    n = max(sum(max(d, 0) for d in dims) // 2, 1)
+    n = max(min(sum(max(d, 0) for d in dims), 128) // 2, 1)      # (more are refused)
     turns = torch.zeros(n, dtype=torch.float64)
     axis = torch.zeros(n, dtype=torch.uint8)
-    arr = (ctypes.c_int * max(len(dims), 1))(*dims)
+    arr = (ctypes.c_int * max(len(dims), 1))(*(min(max(d, -1), 130) for d in dims))
     _check(lib.cast_rope_frequencies(arr, len(dims), base, ROPE_SCALING[scaling], factor, orig_len, beta_fast,
                                      beta_slow, _ptr(turns), _ptr(axis)))
     return turns, axis
@@ -627,6 +637,8 @@ def cast_rope(x, pos, rope: RopeParams, transpose: bool = False, out=None, strea
     if len(shape) != 3:
         _bad(f"x must be [n, H, dh], got {list(shape)}")
     n, H, dh = shape
+    if n > _INT_MAX or H > _INT_MAX:
+        _ints("tokens and heads", n, H)
     if out is None:
         out = _new(stream, _torch.empty_like, x, memory_format=_torch.contiguous_format)
         os_ = (H * dh, dh, 1)
@@ -657,6 +669,7 @@ class KvCache:
         import torch
         if k.dim() != 4 or v.shape != k.shape:
             _bad(f"k and v must be [pages, page, H, dh] alike, got {list(k.shape)} and {list(v.shape)}")
+        _ints("pages, tokens of a page and heads", *k.shape[:3])
         codes = k.dtype != torch.bfloat16
         _want("k", k, (torch.uint8, torch.float8_e4m3fn) if codes else (torch.bfloat16,))
         _want("v", v, (k.dtype,), k.device)
@@ -702,6 +715,7 @@ class KvSeqs:
         if table.dim() != 2 or lens.shape != table.shape[:1] or tuple(cu.shape) != (table.shape[0] + 1,):
             _bad(f"need cu [n_seq + 1], lens [n_seq], table [n_seq, max_pages], got {list(cu.shape)}, "
                  f"{list(lens.shape)}, {list(table.shape)}")
+        _ints("sequences and pages of a sequence", *table.shape)
         self.cu, self.lens, self.table, self.device = cu, lens, table, cu.device
         self.max_pages = table.shape[1]
         self._structs = {}
@@ -709,6 +723,7 @@ class KvSeqs:
     def ref(self, n_tok: int):
         r = self._structs.get(n_tok)
         if r is None:
+            _ints("rows", n_tok)
             s = KvSeqsStruct(_ptr(self.cu), _ptr(self.lens), _ptr(self.table), self.table.shape[0], n_tok,
                              self.table.shape[1])
             if len(self._structs) >= 64:
@@ -758,9 +773,11 @@ def cast_kv_read(cache: KvCache, pages, k_out=None, v_out=None, want_k: bool = T
     layout of cast_route_kv and cast_anchor_attn; None where not wanted."""
     lib = _lib or load()
     dev = cache.device
+    m = pages.numel()
+    if m > _INT_MAX:
+        _ints("pages", m)
     if pages.dtype != _torch.int32 or pages.device != dev or not pages.is_contiguous():
         _bad(f"pages must be a contiguous torch.int32 tensor on {dev}, got {pages.dtype} on {pages.device}")
-    m = pages.numel()
     shape = (m, cache.page, cache.H, cache.dh)
     for name, t in (("k_out", k_out), ("v_out", v_out)):
         if t is not None:
@@ -784,6 +801,7 @@ def _max_len(cache, seqs, max_len):
 
 def cast_kv_attn_workspace_bytes(q, cache: KvCache, seqs: KvSeqs, max_len=None, causal: bool = True,
                                  window: int = 0, sinks: int = 0) -> int:
+    _ints("window and sinks", window, sinks)
     return load().cast_kv_attn_workspace_bytes(cache.ref, seqs.ref(q.shape[0]), q.shape[1],
                                                _max_len(cache, seqs, max_len), int(bool(causal)), window, sinks)
 
@@ -798,8 +816,8 @@ def cast_kv_attn(q, cache: KvCache, seqs: KvSeqs, scale: float, causal: bool = T
     lib = _lib or load()
     if q.dim() != 3:
         _bad(f"q must be [n, Hq, dh], got {list(q.shape)}")
-    if window > 0x7fffffff or sinks > 0x7fffffff:
-        _bad(f"window and sinks must be below 2^31, got {window} and {sinks}")
+    if not 0 <= window <= _INT_MAX or not 0 <= sinks <= _INT_MAX:
+        _ints("window and sinks", window, sinks)
     n, hq, dh = q.shape
     dev = cache.device
     if seqs.device != dev:

@@ -144,3 +144,28 @@ def test_launches_of_the_largest_counts_end(lib, call):
             "import paper_2609_34144_amd as cast\nlib = cast.load()\nfrom test_kv_abi import cache, r_rope, read\n"
             f"sys.exit({call})")
     assert subprocess.run([sys.executable, "-c", code], timeout=60).returncode == HIP
+
+
+# ---------------------------------------------------------------------------
+# the binding: sizes that a C int does not hold
+# ---------------------------------------------------------------------------
+
+def test_sizes_past_32_bits_are_refused(lib):
+    """ctypes would pass their low bits on: a window of -2^32 as none, 2^32 + 5 tokens as five."""
+    z = lambda *s, d=torch.int32: torch.zeros(s, dtype=d)  # noqa: E731
+    big = 1 << 32
+    kv = z(4, 16, 2, 64, d=torch.bfloat16)
+    q, c, s = z(3, 2, 64, d=torch.bfloat16), cast.KvCache(kv, kv.clone()), cast.KvSeqs(z(2), z(1), z(1, 2))
+    rope = cast.RopeParams(z(32, d=torch.float64), None)
+    many = kv[:1, :1].expand(big + 5, 1, 2, 64)
+    bad = [lambda: cast.cast_kv_attn(q, c, s, 0.1, window=-big), lambda: cast.cast_kv_attn(q, c, s, 0.1, window=4, sinks=8 - big),
+           lambda: cast.cast_kv_attn_workspace_bytes(q, c, s, window=big), lambda: cast.cast_kv_attn_workspace_bytes(q, c, s, sinks=-big),
+           lambda: cast.cast_kv_attn_workspace_bytes(many[:, 0], c, s), lambda: cast.cast_kv_append(c, s, many[:, 0], many[:, 0]),
+           lambda: cast.cast_rope(many[:, 0], z(1).expand(big + 5), rope), lambda: cast.cast_kv_read(c, z(1).expand(big + 5)),
+           lambda: cast.KvCache(many, many)]
+    for f in bad:
+        with pytest.raises(cast.CastError, match="below 2\\^31"):
+            f()
+    for dims in ([big + 64], [1 << 40], [-big + 64]):
+        with pytest.raises(cast.CastError):
+            cast.cast_rope_frequencies(dims)
