@@ -634,7 +634,7 @@ size_t cast_kv_attn_workspace_bytes(const cast_kv_cache_t* cache, const cast_kv_
  * lse_out  fp32 [n_tok, Hq] device, natural log-sum-exp of the scaled logits, or NULL.
  * max_len  the longest length expected: it sets how finely keys are split, nothing else
  *          (longer sequences are computed, too, in longer pieces).  >= 1.
- * window >= 0 (0: no window), sinks >= 0; scale finite and > 0.
+ * window >= 0 (0: no window), sinks >= 0; 0 < scale <= 2e38.
  * workspace  NULL (every row tile runs whole), or 256-byte aligned with
  *          cast_kv_attn_workspace_bytes(...) of the same arguments; contents need no
  *          initialisation.  Calls that may overlap in time need workspaces of their own.

@@ -752,7 +752,8 @@ cast_status_t cast_kv_attn(const void* q, long long q_stride, int Hq, const cast
                            size_t workspace_bytes, hipStream_t stream) {
   cast_status_t st = kv_attn_sizes(cache, seqs, Hq, max_len, causal, window, sinks);
   if (st != CAST_OK) return st;
-  if (!(scale > 0.0f) || scale > 3.0e38f) return fail(CAST_ERR_SHAPE, "kv_attn: scale must be finite and > 0");
+  if (!(scale > 0.0f) || scale > 2.0e38f)          // (the kernels' scale is log2(e) times that)
+    return fail(CAST_ERR_SHAPE, "kv_attn: scale must be > 0 and at most 2e38");
   if (seqs->n_tok == 0) return CAST_OK;
   st = cache_pointers(cache, "kv_attn");
   if (st == CAST_OK) st = seqs_pointers(seqs, "kv_attn");

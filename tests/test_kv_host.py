@@ -10,7 +10,7 @@ import torch
 
 import paper_2609_34144_amd as cast
 from test_abi import _HAS_GPU
-from test_kv_abi import A, append, cache, rope, seqs
+from test_kv_abi import A, SHAPE, append, attn, cache, rope, seqs
 
 HIP = 6                          # what a launch gives without a GPU
 
@@ -131,6 +131,13 @@ def test_a_stream_of_another_device_is_refused(lib, monkeypatch):
                            (torch.device("cuda", 1), SimpleNamespace(cuda_stream=0x40, device_index=1))):
         with pytest.raises(cast.CastError):
             cast._on(device, stream)
+
+
+def test_scales_whose_logarithmic_form_overflows_are_refused(lib):
+    """The kernels take scale * log2(e), which must be finite."""
+    if _HAS_GPU:
+        pytest.skip("calls with fake pointers run GPU-less only")
+    assert attn(lib, scale=2.5e38) == SHAPE and attn(lib, scale=2.0e38) == HIP and attn(lib, scale=1e-45) == HIP
 
 
 @pytest.mark.parametrize("call", ["r_rope(lib, n=2 ** 31 - 1, H=1, dh=32, xt=32, xh=32, yt=32, yh=32)",
