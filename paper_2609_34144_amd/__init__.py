@@ -90,7 +90,7 @@ class KvSeqsStruct(ctypes.Structure):
 
 
 _lib = None
-_torch = None                     # set by load()
+_torch = _raw_stream = None       # set by load()
 _c = ctypes
 _ll = _c.c_longlong
 _vp, _i, _f, _sz = _c.c_void_p, _c.c_int, _c.c_float, _c.c_size_t
@@ -102,8 +102,8 @@ def load(path: str = LIB_PATH):
     if _lib is not None:
         return _lib
     import torch  # (loads the HIP runtime libcast.so must share)
-    global _torch
-    _torch = torch
+    global _torch, _raw_stream
+    _torch, _raw_stream = torch, _current_raw_stream(torch)
     if not os.path.exists(path):
         raise RuntimeError(f"{path} is not built; run python -m paper_2609_34144_amd.build")
     lib = ctypes.CDLL(path, mode=ctypes.RTLD_LOCAL)
@@ -553,9 +553,15 @@ def _same(name, t, like, dtype):
              f"{list(t.shape)} on {t.device}")
 
 
+def _current_raw_stream(torch):
+    """Function of a device's index that gives the current stream's handle.  Small calls are bound by
+    the host, so it is torch's own raw one (not public) where there is one."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw if raw is not None else lambda index: torch.cuda.current_stream(index).cuda_stream
+
+
 def _on(device, stream):
-    """The stream's handle, after checking that `device` is current (kernels run there).  Small
-    calls are bound by the host, so this takes torch's raw handle rather than a Stream object."""
+    """The stream's handle, after checking that `device` is current (kernels run there)."""
     index = device.index
     if index is None or device.type != "cuda":
         _bad(f"tensors must be on a GPU, got {device}")
@@ -563,7 +569,7 @@ def _on(device, stream):
         _bad(f"tensors are on {device}, the current device is cuda:{_torch.cuda.current_device()}")
     if stream is not None and stream.device_index != index:
         _bad(f"tensors are on {device}, the stream on cuda:{stream.device_index}")
-    return _torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    return _raw_stream(index) if stream is None else stream.cuda_stream
 
 
 def cast_rope_frequencies(axis_dims, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,

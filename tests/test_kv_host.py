@@ -153,6 +153,14 @@ def test_launches_of_the_largest_counts_end(lib, call):
     assert subprocess.run([sys.executable, "-c", code], timeout=60).returncode == HIP
 
 
+def test_the_current_stream_is_found_without_torchs_private_function():
+    streams = {0: SimpleNamespace(cuda_stream=0x40), 1: SimpleNamespace(cuda_stream=0x50)}
+    other = SimpleNamespace(_C=SimpleNamespace(), cuda=SimpleNamespace(current_stream=streams.get))
+    assert [cast._current_raw_stream(other)(i) for i in (0, 1)] == [0x40, 0x50]
+    other._C._cuda_getCurrentRawStream = lambda index: 0x60 + index
+    assert cast._current_raw_stream(other)(1) == 0x61
+
+
 # ---------------------------------------------------------------------------
 # the binding: sizes that a C int does not hold
 # ---------------------------------------------------------------------------
