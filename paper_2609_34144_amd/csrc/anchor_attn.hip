@@ -509,11 +509,7 @@ __global__ __launch_bounds__(kThreads, wide_waves(DH)) void anchor_attn_kernel(A
         pm = max3f(pm, sn[v / 16][v % 16], sn[(v + 1) / 16][(v + 1) % 16]);
       }
       pm = fmaxf(pm, sn[1][15]);
-      const u32x2 sw = __builtin_bit_cast(
-          u32x2, __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, pm),
-                                                  __builtin_bit_cast(unsigned, pm), false, false));
-      const float mx = fmaxf(__builtin_bit_cast(float, sw.x), __builtin_bit_cast(float, sw.y));
-      const float m_cand = fmaxf(m_run, mx * a.sl2);
+      const float m_cand = fmaxf(m_run, half_swap_max(pm) * a.sl2);
       const bool up = m_cand > m_run + kMaxSlack;
       const float m_new = up ? m_cand : m_run;
       const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -558,11 +554,7 @@ __global__ __launch_bounds__(kThreads, wide_waves(DH)) void anchor_attn_kernel(A
       pm = max3f(pm, sn[v / 16][v % 16], sn[(v + 1) / 16][(v + 1) % 16]);
     }
     pm = fmaxf(pm, sn[1][15]);
-    const u32x2 sw = __builtin_bit_cast(
-        u32x2, __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, pm),
-                                                __builtin_bit_cast(unsigned, pm), false, false));
-    const float mx = fmaxf(__builtin_bit_cast(float, sw.x), __builtin_bit_cast(float, sw.y));
-    const float m_cand = fmaxf(m_run, mx * a.sl2);
+    const float m_cand = fmaxf(m_run, half_swap_max(pm) * a.sl2);
     const bool up = m_cand > m_run + kMaxSlack;
     const float m_new = up ? m_cand : m_run;
     const float corr = __builtin_amdgcn_exp2f(m_run - m_new);

@@ -24,6 +24,14 @@ inline size_t align_up(size_t x, size_t a = kWsAlign) { return (x + a - 1) / a *
 __device__ __forceinline__ float bf16lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+// max over lanes l and l ^ 32 (not __builtin_bit_cast(float, s.y): on an element of a vector
+// it reads the vector's first)
+__device__ __forceinline__ float half_swap_max(float x) {
+  typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 s = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return fmaxf(__uint_as_float(s.x), __uint_as_float(s.y));
+}
+
 // ---------------------------------------------------------------------------
 // Routing plan: how the pooled-mean scan is split (shared by the workspace
 // query and the launch so both agree).

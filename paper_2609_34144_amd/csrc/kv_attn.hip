@@ -120,12 +120,6 @@ __device__ __forceinline__ void static_for(F&& f) {
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
-// max over lanes l and l ^ 32 (not __builtin_bit_cast(float, s.y): on an element of a vector
-// it reads the vector's first)
-__device__ __forceinline__ float half_swap_max(float x) {
-  const u32x2 s = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
-  return fmaxf(__uint_as_float(s.x), __uint_as_float(s.y));
-}
 
 // LDS images: chunk c (16 bytes) of tile row r is stored at chunk c ^ swz(r), CPR chunks
 // per row.  K: ds_read_b128 of one chunk by 32 consecutive rows; V: the transposing read's
