@@ -69,15 +69,6 @@ constexpr int kVmcnt0 = 0x0F70;
 // (see softmax).  With 2^8, keys whose logits spread by 6 moved some wave's maximum in nearly
 // every tile (chunks of 64-wide heads 177 us, so 144; the frame over an 8-bit window 167 and 145).
 constexpr float kMaxSlack = 16.0f;
-// It is kept this much above the scores', in log2 units: exponentials start at 2^-46 and reach
-// 2^-30 at most, so those of a row of 2^30 keys (the longest) sum to at most one, and their
-// products with the values to at most the largest value, which may be the type's.  (With the
-// maximum at the scores' own, finite values above 2^111 could give infinite rows.)  What falls
-// below 2^-126 is lost, as ever; that is 2^-80 of the largest exponential, and products below
-// 2^-80 in size.  The exponent's argument is off by 2^-19 at most, an exponential by 2^-19 of itself.
-constexpr float kLead = 46.0f;
-constexpr float kSumBound = 0x1p-30f;   // 2^(kMaxSlack - kLead)
-constexpr float kLeadScale = 0x1p46f;   // 2^kLead
 constexpr float kJoinScale = 0x1p-14f;  // of a piece in a sum of up to 2^14 of them
 // "no key seen yet": below every finite scaled score, so the first visible key moves it
 constexpr float kNoMax = -3.0e38f;
@@ -372,14 +363,30 @@ __device__ __forceinline__ void mask_scores(f32x16 (&sn)[NB], int j0, int hf, Ro
   }
 }
 
+// The running maximum is kept `lead` above the scores', in log2 units, so exponentials start at
+// 2^-lead and reach 2^(kMaxSlack - lead), which is 2^-bits for a sequence of less than 2^bits keys:
+// those of a row sum to less than one, and their products with the values to less than the largest
+// value, which may be the type's.  (With the maximum at the scores' own, finite values above 2^111
+// could give infinite rows.)  What falls below 2^-126 is lost, as ever: 2^-80 of the largest
+// exponential at most, and products below 2^-80 in size (of 2^30 keys; 2^-98 of 4096).  The
+// exponent's argument is off by 2^-20 for up to 2^15 keys, by 2^-19 for more.
+struct Lead {
+  float lead, bound, scale;      // bound 2^(kMaxSlack - lead), scale 2^lead
+};
+__device__ __forceinline__ Lead lead_of(int len) {
+  const int bits = 32 - __clz(len);
+  return Lead{kMaxSlack + (float)bits, __uint_as_float((uint32_t)(127 - bits) << 23),
+              __uint_as_float((uint32_t)(127 + (int)kMaxSlack + bits) << 23)};
+}
+
 // Exponentials of a tile against the running maximum, in place of the scores (a second set
 // would cost the registers of two waves per SIMD at 64-wide heads), packed as P^T operands,
-// and their sum.  A lane's sum of at most kSumBound shows that no score is far above the maximum,
+// and their sum.  A lane's sum of at most the bound shows that no score is far above the maximum,
 // which then may stay; else the scores are formed again, the maximum is taken over the tile, moved, and the sums
 // so far scaled down.
 template <int NB, int ND, class S>
 __device__ __forceinline__ void softmax(f32x16 (&sn)[NB], S&& scores, bf16x8 (&pp)[NB][2], float& m_run, float& l_run,
-                                        f32x16 (&acc)[ND], float sl2) {
+                                        f32x16 (&acc)[ND], float sl2, const Lead& ld) {
   auto exps = [&]() __attribute__((always_inline)) -> float {
     float rs[4];
 #pragma unroll
@@ -391,12 +398,12 @@ __device__ __forceinline__ void softmax(f32x16 (&sn)[NB], S&& scores, bf16x8 (&p
     return (rs[0] + rs[1]) + (rs[2] + rs[3]);
   };
   float sum = exps();
-  if (__ballot(!(sum <= kSumBound)) != 0ull) {
+  if (__ballot(!(sum <= ld.bound)) != 0ull) {
     scores();
     float pm = sn[0][0];
 #pragma unroll
     for (int e = 1; e < NB * 16; ++e) pm = fmaxf(pm, sn[e / 16][e % 16]);
-    const float cand = fmaxf(m_run, fmaf(half_swap_max(pm), sl2, kLead));
+    const float cand = fmaxf(m_run, fmaf(half_swap_max(pm), sl2, ld.lead));
     const bool up = cand > m_run + kMaxSlack;
     const float m_new = up ? cand : m_run;
     const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -537,7 +544,8 @@ __device__ __forceinline__ void finish(const KvAttnArgs& a, const Unit& un, long
   const float l = l_run + __shfl_xor(l_run, 32);
   const bool some = l != 0.0f;               // true for NaN, too
   const float inv = some ? 1.0f / l : 0.0f;
-  const float l2 = some ? (m_run - kLead) + __log2f(l * kLeadScale) : -INFINITY;
+  const Lead ld = lead_of(un.t.len);
+  const float l2 = some ? (m_run - ld.lead) + __log2f(l * ld.scale) : -INFINITY;
   const long long at = (long long)un.z * a.s.n_tok * a.Hq + row;
   if (a.target > 0 && un.z == 0 && hf == 0) a.cuts[row] = un.pieces;
   if (un.pieces > 1) {
@@ -603,6 +611,7 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
   const int p0 = t.off + min(w0, t.n_rows - 1) / a.g, p1 = t.off + min(w0 + 31, t.n_rows - 1) / a.g;
   const RowLimits lim = row_limits(a, t, t.off + tok);
   const KindBounds kb = kind_bounds(a, t.len, p0, p1);
+  const Lead ld = lead_of(t.len);
   bf16x8 qreg[DH / 16];
   {
     const uint16_t* qp = a.q + (long long)(t.beg + tok) * a.qs + hq * DH + 8 * hf;
@@ -769,7 +778,7 @@ __global__ __launch_bounds__(kThreads, DH == 128 ? 2 : DH == 64 ? 3 : 4) void kv
       };
       scores();
       bf16x8 pp[2][2];
-      softmax<2, ND>(sn, scores, pp, m_run, l_run, acc, a.sl2);
+      softmax<2, ND>(sn, scores, pp, m_run, l_run, acc, a.sl2, ld);
       auto rd = [&](int db, int kb, int s2) __attribute__((always_inline)) { return read_v(vt, vb0, db, kb, s2); };
       if (kind == 1 && has_special<2, ND>(rd)) values_special<2, ND>(rd, pp, acc);
       else values<2, ND>(rd, pp, acc);
@@ -831,6 +840,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
   const int p0 = t.off + min(w0, t.n_rows - 1) / a.g, p1 = t.off + min(w0 + 31, t.n_rows - 1) / a.g;
   const RowLimits lim = row_limits(a, t, t.off + tok);
   const KindBounds kb = kind_bounds(a, t.len, p0, p1);
+  const Lead ld = lead_of(t.len);
   bf16x8 qreg[DH / 16];
   {
     const uint16_t* qp = a.q + (long long)(t.beg + tok) * a.qs + hq * DH + 8 * hf;
@@ -1081,7 +1091,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kv_pairs_kernel(KvAttnArgs a)
         softmax<2, ND>(sn, [&]() __attribute__((always_inline)) {
           products(kc, vc, IC<0>{}, [](auto) {});        // K[j] is still there
           mask();
-        }, pp, m_run, l_run, acc, a.sl2);
+        }, pp, m_run, l_run, acc, a.sl2, ld);
         if (kind == 1) {
           const unsigned vb0 = opaque(vbase);
           auto rd = [&](int db, int kb, int s2) __attribute__((always_inline)) { return read_v(vc, vb0, db, kb, s2); };
@@ -1200,6 +1210,7 @@ __global__ __launch_bounds__(kThreads, row_groups(DH)) void kv_rows_kernel(KvAtt
   const int nrows = min(TM, t.n_rows - t.row0);
   const int p0 = t.off + t.row0 / a.g, p1 = t.off + (t.row0 + nrows - 1) / a.g;
   const KindBounds kb = kind_bounds(a, t.len, p0, p1);
+  const Lead ld = lead_of(t.len);
   RowLimits lim;
   bf16x8 qreg[NT];
   const int r = t.row0 + min(l16, nrows - 1);
@@ -1365,11 +1376,11 @@ __global__ __launch_bounds__(kThreads, row_groups(DH)) void kv_rows_kernel(KvAtt
         return (rs[0] + rs[1]) + (rs[2] + rs[3]);
       };
       float sum = exps();
-      if (__ballot(!(sum <= kSumBound)) != 0ull) {
+      if (__ballot(!(sum <= ld.bound)) != 0ull) {
         float pm = sn[0][0];
 #pragma unroll
         for (int e = 1; e < 8 * SUB; ++e) pm = fmaxf(pm, sn[e / 4][e % 4]);
-        const float cand = fmaxf(m_run, fmaf(quarter_max(pm), a.sl2, kLead));
+        const float cand = fmaxf(m_run, fmaf(quarter_max(pm), a.sl2, ld.lead));
         const bool up = cand > m_run + kMaxSlack;
         const float m_new = up ? cand : m_run;
         const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -1460,7 +1471,7 @@ __global__ __launch_bounds__(kThreads, row_groups(DH)) void kv_rows_kernel(KvAtt
     }
     const bool some = lt != 0.0f;                    // true for NaN, too
     o *= some ? 1.0f / lt : 0.0f;
-    const float l2 = some ? (m - kLead) + __log2f(lt * kLeadScale) : -INFINITY;
+    const float l2 = some ? (m - ld.lead) + __log2f(lt * ld.scale) : -INFINITY;
     if (it.pieces > 1) {
       const long long at = ((long long)blockIdx.x * a.wh + hw) * TM + ql;
       *reinterpret_cast<f32x4*>(a.part_o + at * DH + d) = o;
