@@ -519,7 +519,7 @@ cast_status_t cast_rope_frequencies(const int* axis_dims, int n_axes, double bas
  * pos      device int32 [n, n_axes], any values.
  * transpose  0, or 1: turn by -t (same amplitude).  That is the transposed matrix: it
  *          carries the gradient of the rotation, and with amplitude 1 undoes it.
- * n >= 0 (0: nothing is enqueued), H >= 1, dh in {32, 64, 128}; n * H * dh < 2^40.
+ * n >= 0 (0: nothing is enqueued), H >= 1, dh in {32, 64, 128}; n * H < 2^33.
  * Errors: CAST_ERR_NULL, CAST_ERR_SHAPE (sizes, dtype, strides under which the elements
  * of `out` would meet, out == x with other strides, alignment), CAST_ERR_UNSUPPORTED (dh).
  */

@@ -595,7 +595,7 @@ cast_status_t cast_rope(const void* x, int dtype, int n, int H, int dh, long lon
   if (!dh_ok(dh)) return fail(CAST_ERR_UNSUPPORTED, "rope: dh must be 32, 64 or 128 (got %d)", dh);
   if (dtype != 0 && dtype != 1) return fail(CAST_ERR_SHAPE, "rope: dtype must be 0 (fp32) or 1 (bf16)");
   if (transpose != 0 && transpose != 1) return fail(CAST_ERR_SHAPE, "rope: transpose must be 0 or 1");
-  if ((long long)n * H >= (1LL << 33)) return fail(CAST_ERR_UNSUPPORTED, "rope: n * H * dh must stay below 2^40");
+  if ((long long)n * H >= (1LL << 33)) return fail(CAST_ERR_UNSUPPORTED, "rope: n * H must stay below 2^33");
   const long long top = 1LL << 40;
   if (x_token_stride < dh || x_head_stride < dh || out_token_stride < dh || out_head_stride < dh ||
       x_token_stride > top || x_head_stride > top || out_token_stride > top || out_head_stride > top)

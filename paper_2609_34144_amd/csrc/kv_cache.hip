@@ -4,8 +4,9 @@
 // 28160 tokens of 24 heads of 128 channels rotated: 66 us, 5.2 TB/s; 24960 tokens of 12 heads
 // appended in bf16: 62 us, 4.9 TB/s; 15000 tokens of 8 heads in e4m3, half of the channels
 // rotated: 28 us, 3.3 TB/s (the angles and the two passes over a page take as long as the
-// memory), read back as bf16 29 us; 16 e4m3 pages of 3520 tokens of 24 heads read: 171 us,
-// 6.1 TB/s.
+// memory), read back as bf16 29 us; a frame of 1560 tokens of 12 heads as one e4m3 page 17 us
+// (three launches of 7.8, 3.8 and 6.7), sixteen of them 84; 16 e4m3 pages of 3520 tokens of 24
+// heads read: 171 us, 6.1 TB/s.
 #include <algorithm>
 
 #include "kv_device.h"
@@ -126,7 +127,9 @@ __device__ __forceinline__ void rotate_item(const T* x, T* y, int i, int mode, i
 
 // a (cos, sin) of an angle.  Of the rest of a quarter turn, r of [-1/8, 1/8] in turns,
 //   sin(2 pi r) = r (2 pi + P(r^2)),  cos(2 pi r) = 1 + r^2 Q(r^2)
-// with P and Q fitted over that range to less than 1e-8 (2 pi in two parts).  Off by at most
+// with P and Q fitted over that range to less than 1e-8 (2 pi in two parts): least squares on
+// Chebyshev points, the weights multiplied by the errors until these level out (Lawson's
+// algorithm), the coefficients then rounded to fp32.  Off by at most
 // 7.5e-8, about one fp32 step of 1.  v_cos and v_sin of an fp32 angle are off by up to 2.2e-7:
 // they put 18 of the 15 million codes of 15000 tokens of 8 heads on the other side of a
 // rounding, this 9 (means of six caches), and saved 4 of the append's 32 us.
@@ -761,8 +764,10 @@ cast_status_t launch_kv_append(const cast_kv_cache_t& c, const cast_kv_seqs_t& s
     const long long pages = (long long)s.n_tok / c.page + 2ll * s.n_seq;
     // The rows of a part stay in a block's registers.  Where sequences bring many more
     // to longer pages, several blocks share a page and head, at the price of two more launches:
-    // a frame of 1560 tokens and 12 heads that is a page 17 us, 97 with one block each; 4 x
-    // 6240 tokens in such pages 100 and 134; but 2 x 300 in pages of 100 13.5 and 11.
+    // a frame of 1560 tokens and 12 heads that is a page 17 us, 98 with one block each; 4 x
+    // 6240 tokens in such pages 89 and 133, in pages of 12480 94 and 412; 2 x 300 of 8 heads in
+    // pages of 300 13.6 and 22; 64 x 200 in pages of 4096 48 and 45, where the two sides meet;
+    // but 2 x 300 in pages of 100 13.5 and 11.
     // Two heads of K to a block where that leaves a thousand: 15000 tokens of 8 heads in
     // pages of 64 29 us and 25.5; but 8 x 512 tokens 10.8 and 11.4, 2 x 300 in pages of 100 11
     // and 13.
